@@ -261,6 +261,82 @@ size_t psk_decode_state_bytes(const psk_shape* shape);
 int psk_decode_step(const psk_shape* shape, const void* q, const void* k, const void* v, const void* G1,
                     const void* G2, float* state, void* o, float* denom, void* stream);
 
+/* Layer normalisation of rows, forward and backward: the attention calls take Q and K as already normalised
+ * (Section 2.1 applies LayerNorm first), and these calls make them so.  Per row x of C = cols values
+ *   y = (x - mean) rstd * gain + bias,   mean = sum(x) / C,   rstd = 1 / sqrt(sum((x - mean)^2) / C + eps)
+ * and from dY: dX, and summed over all rows dgain = sum dy * (x - mean) rstd, dbias = sum dy.  The backward
+ * forms mean and rstd again from X; nothing is kept from the forward.
+ *   X, Y, dY, dX  DEVICE, storage dtype: rows [n0, n1, n2] of `cols` contiguous values, each tensor with element
+ *                 strides of its own; extents of 1 may have any stride.  Y (dX) may be X (X or dY) itself, with the same
+ *                 strides; otherwise it overlaps nothing, itself neither (PSK_ERR_SHAPE)
+ *   gain, bias    DEVICE fp32 [cols] or NULL (1 and 0)
+ *   dgain, dbias  DEVICE fp32 [cols] or NULL, overwritten; sums in a fixed order: the same bits every time
+ *   workspace     DEVICE scratch for the backward, 16-byte aligned, >= psk_layer_norm_workspace_bytes(shape)
+ *                 (0 for a bad shape); not read if dgain and dbias are NULL
+ * cols from 1 to 8192, fewer than 2^31 rows.  fp32 arithmetic.  No alignment is asked for: rows that do not lie on 16 bytes
+ * are read value by value. */
+typedef struct {
+    int32_t n0, n1, n2, cols;
+    int32_t dtype;              /* psk_dtype */
+    float eps;                  /* >= 0 */
+    int64_t xs[3];              /* element strides of X */
+    int64_t ys[3];              /* ... of Y (forward) or dY (backward) */
+    int64_t zs[3];              /* ... of dX (backward only) */
+} psk_norm_shape;
+size_t psk_layer_norm_workspace_bytes(const psk_norm_shape* shape);
+int psk_layer_norm_fwd(const psk_norm_shape* shape, const void* X, const float* gain, const float* bias, void* Y, void* stream);
+int psk_layer_norm_bwd(const psk_norm_shape* shape, const void* X, const float* gain, const void* dY, void* dX, float* dgain,
+                       float* dbias, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Sliding-window softmax attention with sinks: exact attention over the recent rows, for the layers (or the heads) that
+ * a model keeps exact next to its sketched ones; like those it costs time linear in n, and decodes on a state of
+ * fixed size.  Row i of a sequence of length L (i < L) sees key j if j <= i and (i - j < window or j < sinks):
+ *   s_ij = scale q_i . k_j,  lse_i = log sum_j exp(s_ij),  o_i = sum_j exp(s_ij - lse_i) v_j
+ * `window` >= n is causal attention over the whole sequence.  Rows from L on: o = 0, lse = -inf, gradients 0.
+ * A pair that the mask leaves out counts for nothing, whatever stands in its rows (infinities and NaN too).
+ *   Q, O, dO, dQ   DEVICE [B, H, n, h], strides q_stride_*;  K, V, dK, dV   DEVICE [B, Hkv, n, h], strides kv_stride_*
+ *                  (elements, last dimension contiguous, multiples of 16 bytes; the stride of an extent of 1 is not
+ *                  looked at); rows must not overlap (PSK_ERR_SHAPE), outputs overlap no input
+ *   lse            DEVICE [B, H, n] fp32, written by the forward, read by the backward
+ *   lengths        DEVICE [B] int32 or NULL (all n); clamped to 0 .. n
+ *   workspace      DEVICE scratch, 256-byte aligned, >= psk_window_workspace_bytes(shape, for_backward) (0 for a bad
+ *                  shape); its first word is the status that psk_check() reads
+ * Query head h reads key head h / (H / Hkv); dK and dV are summed over the query heads that share one, in a fixed
+ * order.  h = 64, any n >= 1, window >= 1, sinks >= 0, scale > 0.  CUDA cores, fp32 arithmetic.
+ * The backward takes D_i = do_i . o_i from the stored O. */
+typedef struct {
+    int32_t B, H, Hkv, n, h, window, sinks;
+    int32_t dtype;              /* psk_dtype */
+    int32_t path;               /* psk_path */
+    float scale;
+    int64_t q_stride_b, q_stride_h, q_stride_n;
+    int64_t kv_stride_b, kv_stride_h, kv_stride_n;
+} psk_window_shape;
+size_t psk_window_workspace_bytes(const psk_window_shape* shape, int for_backward);
+int psk_window_attn_fwd(const psk_window_shape* shape, const void* Q, const void* K, const void* V, const int32_t* lengths,
+                        void* O, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+int psk_window_attn_bwd(const psk_window_shape* shape, const void* Q, const void* K, const void* V, const int32_t* lengths,
+                        const void* O, const float* lse, const void* dO, void* dQ, void* dK, void* dV, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
+/* The same attention one token at a time.  A sequence's cache has sinks + window slots per key head: position p < sinks lies
+ * in slot p, a later one in slot sinks + (p - sinks) mod window.
+ *   Kc, Vc     DEVICE [B, Hkv, sinks + window, h] storage dtype, contiguous, owned by the caller
+ *              (psk_window_cache_bytes() each; 0 for a bad shape)
+ * psk_window_cache_fill writes the slots of a prompt's positions (K, V, lengths as for the forward; of positions that share
+ * a slot the last) and leaves all others as they are.
+ * psk_window_decode_step takes the token of each sequence at its position t = positions[b] (DEVICE [B] int32): writes
+ * k, v [B, Hkv, h] into the position's slot and attends with q [B, H, h] over the slots that positions 0 .. t have written:
+ * o [B, H, h] is row t of psk_window_attn_fwd when the cache holds the positions before t.  All contiguous DEVICE
+ * arrays of the shape's dtype.  A negative position marks an idle place: o = 0, its cache is not touched.  Positions are
+ * counted from the sequence's start and go on past the window, to 2^31 - 1.  Of the shape n and the strides are not read.  CUDA-core
+ * kernel, fp32 arithmetic, for either dtype; no workspace, one launch. */
+size_t psk_window_cache_bytes(const psk_window_shape* shape);
+int psk_window_cache_fill(const psk_window_shape* shape, const void* K, const void* V, const int32_t* lengths, void* Kc, void* Vc,
+                          void* stream);
+int psk_window_decode_step(const psk_window_shape* shape, const void* q, const void* k, const void* v, const int32_t* positions,
+                           void* Kc, void* Vc, void* o, void* stream);
+
 /* Synchronises `stream`, then reports PSK_ERR_TIMEOUT if a kernel of the last call that
  * used `workspace` abandoned a bounded wait, PSK_ERR_CUDA if the stream is in error,
  * else PSK_OK.  Never traps. */

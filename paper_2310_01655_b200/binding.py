@@ -6,7 +6,7 @@ import importlib
 import os
 import sysconfig
 import warnings
-from ctypes import c_int, c_int32, c_int64, c_size_t, c_void_p, c_char_p, POINTER, Structure, byref
+from ctypes import c_float, c_int, c_int32, c_int64, c_size_t, c_void_p, c_char_p, POINTER, Structure, byref
 
 import torch
 
@@ -32,11 +32,27 @@ class Shape(Structure):
                 ("g_heads", c_int32), ("path", c_int32), ("flags", c_int32), ("seq_segments", c_int32)]
 
 
+class NormShape(Structure):
+    """Mirror of `psk_norm_shape`."""
+    _fields_ = [("n0", c_int32), ("n1", c_int32), ("n2", c_int32), ("cols", c_int32), ("dtype", c_int32), ("eps", c_float),
+                ("xs", c_int64 * 3), ("ys", c_int64 * 3), ("zs", c_int64 * 3)]
+
+
+class WindowShape(Structure):
+    """Mirror of `psk_window_shape`."""
+    _fields_ = [("B", c_int32), ("H", c_int32), ("Hkv", c_int32), ("n", c_int32), ("h", c_int32), ("window", c_int32), ("sinks", c_int32),
+                ("dtype", c_int32), ("path", c_int32), ("scale", c_float),
+                ("q_stride_b", c_int64), ("q_stride_h", c_int64), ("q_stride_n", c_int64),
+                ("kv_stride_b", c_int64), ("kv_stride_h", c_int64), ("kv_stride_n", c_int64)]
+
+
 _lib = None
 _fast = None          # the native marshalling module (csrc/psk_binding.cpp), bound to _lib's entry points
 _FAST_ENTRIES = ("psk_workspace_bytes", "psk_causal_attn_fwd", "psk_causal_attn_bwd", "psk_lt_multiply_workspace_bytes",
                  "psk_lt_multiply", "psk_lt_multiply_bf16_workspace_bytes", "psk_lt_multiply_bf16", "psk_decode_step",
-                 "psk_learned_workspace_bytes", "psk_learned_attn_fwd", "psk_learned_attn_bwd")
+                 "psk_learned_workspace_bytes", "psk_learned_attn_fwd", "psk_learned_attn_bwd", "psk_layer_norm_workspace_bytes",
+                 "psk_layer_norm_fwd", "psk_layer_norm_bwd", "psk_window_workspace_bytes", "psk_window_attn_fwd", "psk_window_attn_bwd",
+                 "psk_window_cache_fill", "psk_window_decode_step")
 
 
 def library_path() -> str:
@@ -96,6 +112,25 @@ def lib():
     L.psk_learned_attn_fwd.argtypes = [P] + [c_void_p] * 7 + [c_size_t, c_void_p]
     L.psk_learned_attn_bwd.restype = c_int
     L.psk_learned_attn_bwd.argtypes = [P] + [c_void_p] * 12 + [c_size_t, c_void_p]
+    N, W = POINTER(NormShape), POINTER(WindowShape)
+    L.psk_layer_norm_workspace_bytes.restype = c_size_t
+    L.psk_layer_norm_workspace_bytes.argtypes = [N]
+    L.psk_layer_norm_fwd.restype = c_int
+    L.psk_layer_norm_fwd.argtypes = [N] + [c_void_p] * 5
+    L.psk_layer_norm_bwd.restype = c_int
+    L.psk_layer_norm_bwd.argtypes = [N] + [c_void_p] * 7 + [c_size_t, c_void_p]
+    L.psk_window_workspace_bytes.restype = c_size_t
+    L.psk_window_workspace_bytes.argtypes = [W, c_int]
+    L.psk_window_attn_fwd.restype = c_int
+    L.psk_window_attn_fwd.argtypes = [W] + [c_void_p] * 7 + [c_size_t, c_void_p]
+    L.psk_window_attn_bwd.restype = c_int
+    L.psk_window_attn_bwd.argtypes = [W] + [c_void_p] * 11 + [c_size_t, c_void_p]
+    L.psk_window_cache_bytes.restype = c_size_t
+    L.psk_window_cache_bytes.argtypes = [W]
+    L.psk_window_cache_fill.restype = c_int
+    L.psk_window_cache_fill.argtypes = [W] + [c_void_p] * 6
+    L.psk_window_decode_step.restype = c_int
+    L.psk_window_decode_step.argtypes = [W] + [c_void_p] * 8
     L.psk_profile_enable.restype = c_int
     L.psk_profile_enable.argtypes = [c_int]
     L.psk_profile_count.restype = c_int
@@ -120,6 +155,7 @@ class _NoNative:
         return None
 
     attn_fwd = attn_bwd = learned_fwd = learned_bwd = lt_multiply = decode_step = _none
+    layer_norm_fwd = layer_norm_bwd = window_attn_fwd = window_attn_bwd = window_cache_fill = window_decode_step = _none
 
 
 def _native():
@@ -537,3 +573,241 @@ def decode_step(q, k, v, G1, G2, state):
     if st != 0:
         raise PskError(st, "psk_decode_step")
     return o, den
+
+
+# ---- layer normalisation; sliding-window attention and its cache ----
+# (these calls run on their tensors' device, on that device's current stream, whichever device is current)
+
+def _one_device(where, x, *ts):
+    _require_cuda(x, *ts)
+    for t in ts:
+        if t is not None and t.device != x.device:
+            raise ValueError("%s: all tensors must be on one device" % where)
+
+
+def _storage(where, x):
+    if x.dtype not in _DTYPES:
+        raise ValueError("%s: unsupported storage dtype %s" % (where, x.dtype))
+
+
+def _norm_rows(where, x):
+    """Extents and strides of the leading dimensions, as three."""
+    if not 1 <= x.dim() <= 4 or (x.shape[-1] != 1 and x.stride(-1) != 1):
+        raise ValueError("%s expects rows [.., cols] of at most three leading dimensions and a contiguous last one" % where)
+    fill = 4 - x.dim()
+    return [1] * fill + list(x.shape[:-1]), [0] * fill + list(x.stride()[:-1])
+
+
+def _norm_shape(where, x, eps, *others):
+    for t in others:
+        if t.shape != x.shape or t.dtype != x.dtype:
+            raise ValueError("%s: all row tensors must have one shape and dtype" % where)
+    rows = [_norm_rows(where, t) for t in (x,) + others]
+    n = rows[0][0]
+    if max(n) > 2**31 - 1 or x.shape[-1] > 2**31 - 1:
+        raise PskError(-3, where)
+    s = NormShape(n[0], n[1], n[2], x.shape[-1], _DTYPES[x.dtype], eps)
+    for field, (_, strides) in zip(("xs", "ys", "zs"), rows):
+        setattr(s, field, (c_int64 * 3)(*strides))
+    return s
+
+
+def _norm_params(where, x, *ps):
+    for p in ps:
+        if p is not None and (p.dtype != torch.float32 or p.shape != (x.shape[-1],) or not p.is_contiguous()):
+            raise ValueError("%s: gain and bias must be contiguous fp32 [cols] tensors" % where)
+
+
+def _bytes_workspace(where, need, workspace, x):
+    """The caller's scratch (uint8), or one of `need` bytes; (None, 0) if the library has to report what is wrong."""
+    if workspace is not None and (workspace.dtype != torch.uint8 or not workspace.is_contiguous()):
+        raise ValueError("%s: workspace must be a contiguous uint8 tensor" % where)
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+    return workspace, workspace.numel() if workspace is not None and need else 0
+
+
+def layer_norm_fwd(X, gain=None, bias=None, eps=1e-6, out=None):
+    """psk_layer_norm_fwd: (X - mean) / sqrt(var + eps) * gain + bias over the last dimension; X [.., cols] with at most
+    three leading dimensions of any strides, gain and bias fp32 [cols] or None.  `out` may be X."""
+    res = (_fast or _native()).layer_norm_fwd(X, gain, bias, eps, out)
+    if res is not None:
+        return _result(res, "psk_layer_norm_fwd")
+    where = "layer_norm_fwd"
+    _one_device(where, X, gain, bias, out)
+    _storage(where, X)
+    _norm_params(where, X, gain, bias)
+    with torch.cuda.device(X.device):
+        Y = _empty_like(X) if out is None else out
+        shp = _norm_shape(where, X, eps, Y)
+        st = lib().psk_layer_norm_fwd(byref(shp), _ptr(X), _ptr(gain), _ptr(bias), _ptr(Y), _stream())
+    if st != 0:
+        raise PskError(st, "psk_layer_norm_fwd")
+    return Y
+
+
+def layer_norm_workspace_bytes(X) -> int:
+    """psk_layer_norm_workspace_bytes: the backward's scratch for rows of X's shape."""
+    n, _ = _norm_rows("layer_norm_workspace_bytes", X)
+    # (rows side by side: the strides do not change the size)
+    s = (n[1] * n[2] * X.shape[-1], n[2] * X.shape[-1], X.shape[-1])
+    shp = NormShape(n[0], n[1], n[2], X.shape[-1], _DTYPES[X.dtype], 0.0, s, s, s)
+    return int(lib().psk_layer_norm_workspace_bytes(byref(shp)))
+
+
+def layer_norm_bwd(X, gain, dY, eps=1e-6, params=True, workspace=None, out=None):
+    """psk_layer_norm_bwd: returns (dX, dgain, dbias) from the forward's X and gain; dgain and dbias (fp32) are None
+    with params = False.  `out` (dX) may be X or dY."""
+    res = (_fast or _native()).layer_norm_bwd(X, gain, dY, eps, params, workspace, out)
+    if res is not None:
+        return _result(res, "psk_layer_norm_bwd")
+    where = "layer_norm_bwd"
+    _one_device(where, X, gain, dY, workspace, out)
+    _storage(where, X)
+    _norm_params(where, X, gain)
+    with torch.cuda.device(X.device):
+        dX = _empty_like(X) if out is None else out
+        shp = _norm_shape(where, X, eps, dY, dX)
+        dgain = dbias = None
+        ws, nbytes = None, 0
+        if params:
+            dgain, dbias = (torch.empty(X.shape[-1], dtype=torch.float32, device=X.device) for _ in range(2))
+            ws, nbytes = _bytes_workspace(where, int(lib().psk_layer_norm_workspace_bytes(byref(shp))), workspace, X)
+        st = lib().psk_layer_norm_bwd(byref(shp), _ptr(X), _ptr(gain), _ptr(dY), _ptr(dX), _ptr(dgain), _ptr(dbias), _ptr(ws), nbytes, _stream())
+    if st != 0:
+        raise PskError(st, "psk_layer_norm_bwd")
+    return dX, dgain, dbias
+
+
+def _window_scale(scale, h):
+    return h ** -0.5 if scale is None else scale
+
+
+def make_window_shape(Q, K, window, sinks=0, scale=None, path=PATH_AUTO) -> WindowShape:
+    """Shape descriptor for [B,H,n,h] queries and [B,Hkv,n,h] keys (whose strides stand for all tensors of their side)."""
+    for x in (Q, K):
+        if x.dim() != 4 or x.stride(3) != 1:
+            raise ValueError("expected [B,H,n,h] and [B,Hkv,n,h] tensors with a contiguous last dimension")
+    _storage("window attention", Q)
+    if K.dtype != Q.dtype or (K.shape[0], K.shape[2], K.shape[3]) != (Q.shape[0], Q.shape[2], Q.shape[3]):
+        raise ValueError("window attention: queries and keys must agree in dtype, batch, length and head dimension")
+    B, H, n, h = Q.shape
+    return WindowShape(B, H, K.shape[1], n, h, window, sinks, _DTYPES[Q.dtype], path, _window_scale(scale, h), *Q.stride()[:3], *K.stride()[:3])
+
+
+def window_workspace_bytes(shape: WindowShape, for_backward: bool) -> int:
+    return int(lib().psk_window_workspace_bytes(byref(shape), 1 if for_backward else 0))
+
+
+def _per_sequence(name, x, t):
+    if t is not None and (t.dtype != torch.int32 or t.shape != (x.shape[0],) or not t.is_contiguous()):
+        raise ValueError("%s must be a contiguous int32 [B] tensor" % name)
+
+
+def _row_statistics(shape, lse):
+    if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.numel() != shape.B * shape.H * shape.n):
+        raise ValueError("lse must be a contiguous fp32 [B,H,n] tensor")
+
+
+def window_attn_fwd(Q, K, V, window, sinks=0, scale=None, lengths=None, path=PATH_AUTO, workspace=None, out=None, lse=None):
+    """psk_window_attn_fwd: softmax attention of every row over the `window` rows up to its own and the first `sinks` rows;
+    Q [B,H,n,64], K and V [B,Hkv,n,64], scale 1/sqrt(h) unless given, lengths int32 [B] or None; returns (O, lse)."""
+    res = (_fast or _native()).window_attn_fwd(Q, K, V, window, sinks, 0.125 if scale is None else scale, lengths, path, workspace, out, lse)
+    if res is not None:
+        return _result(res, "psk_window_attn_fwd")
+    where = "window_attn_fwd"
+    _one_device(where, Q, K, V, lengths, workspace, out, lse)
+    _same_layout(K, V)
+    _same_layout(Q, out)
+    _per_sequence("lengths", Q, lengths)
+    shp = make_window_shape(Q, K, window, sinks, scale, path)
+    _row_statistics(shp, lse)
+    with torch.cuda.device(Q.device):
+        O = _empty_like(Q) if out is None else out
+        if lse is None:
+            lse = torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device)
+        ws, nbytes = _bytes_workspace(where, window_workspace_bytes(shp, False), workspace, Q)
+        st = lib().psk_window_attn_fwd(byref(shp), _ptr(Q), _ptr(K), _ptr(V), _ptr(lengths), _ptr(O), _ptr(lse), _ptr(ws), nbytes, _stream())
+    if st != 0:
+        raise PskError(st, "psk_window_attn_fwd")
+    return O, lse
+
+
+def window_attn_bwd(Q, K, V, O, lse, dO, window, sinks=0, scale=None, lengths=None, path=PATH_AUTO, workspace=None, out=None):
+    """psk_window_attn_bwd: returns (dQ, dK, dV) from the forward's inputs and outputs."""
+    res = (_fast or _native()).window_attn_bwd(Q, K, V, O, lse, dO, window, sinks, 0.125 if scale is None else scale, lengths, path, workspace, out)
+    if res is not None:
+        return _result(res, "psk_window_attn_bwd")
+    where = "window_attn_bwd"
+    dQ, dK, dV = out if out is not None else (None, None, None)
+    _one_device(where, Q, K, V, O, lse, dO, lengths, workspace, dQ, dK, dV)
+    _same_layout(K, V, dK, dV)
+    _same_layout(Q, O, dO, dQ)
+    _per_sequence("lengths", Q, lengths)
+    shp = make_window_shape(Q, K, window, sinks, scale, path)
+    _row_statistics(shp, lse)
+    with torch.cuda.device(Q.device):
+        if out is None:
+            dQ, dK, dV = _empty_like(Q), _empty_like(K), _empty_like(K)
+        ws, nbytes = _bytes_workspace(where, window_workspace_bytes(shp, True), workspace, Q)
+        st = lib().psk_window_attn_bwd(byref(shp), _ptr(Q), _ptr(K), _ptr(V), _ptr(lengths), _ptr(O), _ptr(lse), _ptr(dO), _ptr(dQ), _ptr(dK),
+                                       _ptr(dV), _ptr(ws), nbytes, _stream())
+    if st != 0:
+        raise PskError(st, "psk_window_attn_bwd")
+    return dQ, dK, dV
+
+
+def window_cache(B, Hkv, window, sinks=0, dtype=torch.bfloat16, device="cuda", h=64):
+    """Zeroed cache (Kc, Vc) for window_decode_step: [B, Hkv, sinks + window, h] each."""
+    return tuple(torch.zeros((B, Hkv, sinks + window, h), dtype=dtype, device=device) for _ in range(2))
+
+
+def _check_cache(where, x, Hkv, Kc, Vc, window, sinks):
+    for c in (Kc, Vc):
+        if c.dtype != x.dtype or tuple(c.shape) != (x.shape[0], Hkv, sinks + window, x.shape[-1]) or not c.is_contiguous():
+            raise ValueError("%s: Kc and Vc must be contiguous [B, Hkv, sinks + window, h] tensors of the keys' dtype" % where)
+
+
+def window_cache_fill(K, V, Kc, Vc, window, sinks=0, lengths=None):
+    """psk_window_cache_fill: writes what row n (or lengths[b]) would see of a prompt's K, V [B,Hkv,n,64] into the cache."""
+    res = (_fast or _native()).window_cache_fill(K, V, Kc, Vc, window, sinks, lengths)
+    if res is not None:
+        _result(res, "psk_window_cache_fill")
+        return
+    where = "window_cache_fill"
+    _one_device(where, K, V, Kc, Vc, lengths)
+    _same_layout(K, V)
+    _per_sequence("lengths", K, lengths)
+    shp = make_window_shape(K, K, window, sinks)
+    _check_cache(where, K, K.shape[1], Kc, Vc, window, sinks)
+    with torch.cuda.device(K.device):
+        st = lib().psk_window_cache_fill(byref(shp), _ptr(K), _ptr(V), _ptr(lengths), _ptr(Kc), _ptr(Vc), _stream())
+    if st != 0:
+        raise PskError(st, "psk_window_cache_fill")
+
+
+def window_decode_step(q, k, v, Kc, Vc, positions, window, sinks=0, scale=None, out=None):
+    """psk_window_decode_step: q [B,H,64], k and v [B,Hkv,64] of one token per sequence at `positions` (int32 [B], negative: idle);
+    updates the cache in place and returns o [B,H,64]."""
+    res = (_fast or _native()).window_decode_step(q, k, v, Kc, Vc, positions, window, sinks, 0.125 if scale is None else scale, out)
+    if res is not None:
+        return _result(res, "psk_window_decode_step")
+    where = "window_decode_step"
+    _one_device(where, q, k, v, Kc, Vc, positions, out)
+    _storage(where, q)
+    for t in (q, k, v):
+        if t.dim() != 3 or not t.is_contiguous() or t.dtype != q.dtype:
+            raise ValueError("window_decode_step expects contiguous [B,H,h] and [B,Hkv,h] tensors of one dtype")
+    if k.shape != v.shape or (k.shape[0], k.shape[2]) != (q.shape[0], q.shape[2]):
+        raise ValueError("window_decode_step: q [B,H,h] and k, v [B,Hkv,h] must agree")
+    _same_layout(q, out)
+    _per_sequence("positions", q, positions)
+    _check_cache(where, q, k.shape[1], Kc, Vc, window, sinks)
+    B, H, h = q.shape
+    shp = WindowShape(B, H, k.shape[1], 1, h, window, sinks, _DTYPES[q.dtype], PATH_AUTO, _window_scale(scale, h), 0, 0, 0, 0, 0, 0)
+    with torch.cuda.device(q.device):
+        o = torch.empty_like(q) if out is None else out
+        st = lib().psk_window_decode_step(byref(shp), _ptr(q), _ptr(k), _ptr(v), _ptr(positions), _ptr(Kc), _ptr(Vc), _ptr(o), _stream())
+    if st != 0:
+        raise PskError(st, "psk_window_decode_step")
+    return o

@@ -10,6 +10,7 @@
 #include <ATen/ATen.h>
 #include <ATen/cuda/CUDAContextLight.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -30,6 +31,14 @@ struct Api {
     decltype(&psk_learned_workspace_bytes) learned_bytes;
     decltype(&psk_learned_attn_fwd) learned_fwd;
     decltype(&psk_learned_attn_bwd) learned_bwd;
+    decltype(&psk_layer_norm_workspace_bytes) norm_bytes;
+    decltype(&psk_layer_norm_fwd) norm_fwd;
+    decltype(&psk_layer_norm_bwd) norm_bwd;
+    decltype(&psk_window_workspace_bytes) window_bytes;
+    decltype(&psk_window_attn_fwd) window_fwd;
+    decltype(&psk_window_attn_bwd) window_bwd;
+    decltype(&psk_window_cache_fill) window_fill;
+    decltype(&psk_window_decode_step) window_step;
 } api;
 
 using at::Tensor;
@@ -252,6 +261,217 @@ PyObject* learned_bwd(PyObject* const* a, Py_ssize_t n) {
     return t;
 }
 
+// ---- layer normalisation, sliding-window attention: all tensors on one device, which need not be the current one ----
+
+bool on_device_of(const Tensor& a, const Tensor* t) { return t == nullptr || (t->is_cuda() && t->device() == a.device()); }
+bool number(PyObject* o, double& v) {
+    if (!PyFloat_Check(o) && !PyLong_Check(o)) return false;
+    v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) { PyErr_Clear(); return false; }
+    return true;
+}
+bool storage_type(const Tensor& x) { return x.scalar_type() == at::kFloat || x.scalar_type() == at::kBFloat16; }
+int dtype_of(const Tensor& x) { return x.scalar_type() == at::kFloat ? PSK_F32 : PSK_BF16; }
+// rows [.., cols] of at most three leading dimensions
+bool rows_of(const Tensor& x, int32_t (&n)[3], int64_t (&s)[3]) {
+    const int64_t d = x.dim() - 1;
+    if (d < 0 || d > 3 || (x.size(d) != 1 && x.stride(d) != 1)) return false;
+    for (int i = 0; i < 3; ++i) {
+        const int64_t k = i - (3 - d);
+        if (k >= 0 && x.size(k) > INT32_MAX) return false;
+        n[i] = k < 0 ? 1 : (int32_t)x.size(k);
+        s[i] = k < 0 ? 0 : x.stride(k);
+    }
+    return x.size(d) <= INT32_MAX;
+}
+bool param_ok(const Tensor& x, const Tensor* p) {
+    return p == nullptr || (on_device_of(x, p) && p->scalar_type() == at::kFloat && p->dim() == 1 && p->size(0) == x.size(-1) && p->is_contiguous());
+}
+
+// (X, gain, bias, eps, out) -> Y
+PyObject* layer_norm_fwd(PyObject* const* a, Py_ssize_t n) {
+    if (n != 5) Py_RETURN_NONE;
+    bool ok = true;
+    double eps;
+    const Tensor *X = cuda_tensor(a[0], ok), *gain = tensor(a[1], ok), *bias = tensor(a[2], ok), *out = tensor(a[4], ok);
+    if (!ok || !number(a[3], eps) || !storage_type(*X) || X->dim() < 1 || !param_ok(*X, gain) || !param_ok(*X, bias)) Py_RETURN_NONE;
+    if (out != nullptr && (!on_device_of(*X, out) || out->scalar_type() != X->scalar_type() || out->sizes() != X->sizes())) Py_RETURN_NONE;
+    psk_norm_shape s{};
+    int32_t e[3];
+    if (!rows_of(*X, e, s.xs)) Py_RETURN_NONE;
+    c10::cuda::CUDAGuard guard(X->device());
+    Tensor Y = out != nullptr ? *out : empty_as(*X);
+    if (!rows_of(Y, e, s.ys)) Py_RETURN_NONE;
+    s.n0 = e[0]; s.n1 = e[1]; s.n2 = e[2]; s.cols = (int32_t)X->size(-1); s.dtype = dtype_of(*X); s.eps = (float)eps;
+    int st;
+    void* cs = stream();
+    PSK_NO_GIL(st, api.norm_fwd(&s, ptr(X), (const float*)ptr(gain), (const float*)ptr(bias), Y.data_ptr(), cs));
+    if (st != 0) return status_of(st);
+    return THPVariable_Wrap(std::move(Y));
+}
+
+// (X, gain, dY, eps, params, workspace, out) -> (dX, dgain, dbias)
+PyObject* layer_norm_bwd(PyObject* const* a, Py_ssize_t n) {
+    if (n != 7) Py_RETURN_NONE;
+    bool ok = true;
+    double eps;
+    const Tensor *X = cuda_tensor(a[0], ok), *gain = tensor(a[1], ok), *dY = cuda_tensor(a[2], ok), *ws = tensor(a[5], ok), *out = tensor(a[6], ok);
+    if (!ok || !number(a[3], eps) || !PyBool_Check(a[4]) || !storage_type(*X) || X->dim() < 1 || !param_ok(*X, gain)) Py_RETURN_NONE;
+    const bool params = a[4] == Py_True;
+    for (const Tensor* t : {dY, out})
+        if (t != nullptr && (!on_device_of(*X, t) || t->scalar_type() != X->scalar_type() || t->sizes() != X->sizes())) Py_RETURN_NONE;
+    if (ws != nullptr && (!on_device_of(*X, ws) || ws->scalar_type() != at::kByte || !ws->is_contiguous())) Py_RETURN_NONE;
+    psk_norm_shape s{};
+    int32_t e[3];
+    if (!rows_of(*X, e, s.xs) || !rows_of(*dY, e, s.ys)) Py_RETURN_NONE;
+    c10::cuda::CUDAGuard guard(X->device());
+    Tensor dX = out != nullptr ? *out : empty_as(*X);
+    if (!rows_of(dX, e, s.zs)) Py_RETURN_NONE;
+    s.n0 = e[0]; s.n1 = e[1]; s.n2 = e[2]; s.cols = (int32_t)X->size(-1); s.dtype = dtype_of(*X); s.eps = (float)eps;
+    Tensor dg, db;
+    Scratch w;
+    if (params) {
+        dg = empty({X->size(-1)}, at::kFloat, *X);
+        db = empty({X->size(-1)}, at::kFloat, *X);
+        w.take(ws, api.norm_bytes(&s), 0, *X);
+    }
+    int st;
+    void* cs = stream();
+    PSK_NO_GIL(st, api.norm_bwd(&s, ptr(X), (const float*)ptr(gain), ptr(dY), dX.data_ptr(), params ? (float*)dg.data_ptr() : nullptr,
+                                params ? (float*)db.data_ptr() : nullptr, w.p, w.n, cs));
+    if (st != 0) return status_of(st);
+    PyObject* t = PyTuple_New(3);
+    PyTuple_SET_ITEM(t, 0, THPVariable_Wrap(std::move(dX)));
+    for (int i = 1; i < 3; ++i) {
+        if (params) { PyTuple_SET_ITEM(t, i, THPVariable_Wrap(i == 1 ? dg : db)); }
+        else { Py_INCREF(Py_None); PyTuple_SET_ITEM(t, i, Py_None); }
+    }
+    return t;
+}
+
+// Q [B,H,n,h], K and V [B,Hkv,n,h] of one layout, on one device; lengths [B] int32 or none
+bool window_shape(const Tensor& Q, const Tensor& K, const Tensor* V, const Tensor* lengths, int window, int sinks, double scale, int path, psk_window_shape* s) {
+    if (Q.dim() != 4 || K.dim() != 4 || !storage_type(Q) || K.scalar_type() != Q.scalar_type() || !on_device_of(Q, &K) || !on_device_of(Q, V)) return false;
+    if (V != nullptr && !same_layout(K, V)) return false;
+    if (K.size(0) != Q.size(0) || K.size(2) != Q.size(2) || K.size(3) != Q.size(3) || Q.stride(3) != 1 || K.stride(3) != 1) return false;
+    for (int i = 0; i < 4; ++i) if (Q.size(i) > INT32_MAX || K.size(i) > INT32_MAX) return false;
+    if (lengths != nullptr && (!on_device_of(Q, lengths) || lengths->scalar_type() != at::kInt || lengths->dim() != 1 || lengths->size(0) != Q.size(0) ||
+                               !lengths->is_contiguous())) return false;
+    *s = psk_window_shape{(int32_t)Q.size(0), (int32_t)Q.size(1), (int32_t)K.size(1), (int32_t)Q.size(2), (int32_t)Q.size(3), window, sinks, dtype_of(Q), path,
+                          (float)scale, Q.stride(0), Q.stride(1), Q.stride(2), K.stride(0), K.stride(1), K.stride(2)};
+    return true;
+}
+bool bytes_ok(const Tensor& x, const Tensor* ws) {
+    return ws == nullptr || (on_device_of(x, ws) && ws->scalar_type() == at::kByte && ws->is_contiguous());
+}
+
+// (Q, K, V, window, sinks, scale, lengths, path, workspace, out, lse) -> (O, lse)
+PyObject* window_attn_fwd(PyObject* const* a, Py_ssize_t n) {
+    if (n != 11) Py_RETURN_NONE;
+    bool ok = true;
+    double scale;
+    const Tensor *Q = cuda_tensor(a[0], ok), *K = cuda_tensor(a[1], ok), *V = cuda_tensor(a[2], ok), *len = tensor(a[6], ok), *ws = tensor(a[8], ok);
+    const Tensor *out = tensor(a[9], ok), *lse = tensor(a[10], ok);
+    const int window = integer(a[3], ok), sinks = integer(a[4], ok), path = integer(a[7], ok);
+    psk_window_shape s;
+    if (!ok || !number(a[5], scale) || !window_shape(*Q, *K, V, len, window, sinks, scale, path, &s) || !bytes_ok(*Q, ws)) Py_RETURN_NONE;
+    if (out != nullptr && (!on_device_of(*Q, out) || !same_layout(*Q, out))) Py_RETURN_NONE;
+    if (lse != nullptr && (!on_device_of(*Q, lse) || lse->scalar_type() != at::kFloat || !lse->is_contiguous() || lse->numel() != (int64_t)s.B * s.H * s.n)) Py_RETURN_NONE;
+    c10::cuda::CUDAGuard guard(Q->device());
+    Tensor O = out != nullptr ? *out : empty_as(*Q), l = lse != nullptr ? *lse : empty({s.B, s.H, s.n}, at::kFloat, *Q);
+    Scratch w;
+    w.take(ws, api.window_bytes(&s, 0), 0, *Q);
+    int st;
+    void* cs = stream();
+    PSK_NO_GIL(st, api.window_fwd(&s, ptr(Q), ptr(K), ptr(V), (const int32_t*)ptr(len), O.data_ptr(), (float*)l.data_ptr(), w.p, w.n, cs));
+    if (st != 0) return status_of(st);
+    return tuple2(std::move(O), std::move(l));
+}
+
+// (Q, K, V, O, lse, dO, window, sinks, scale, lengths, path, workspace, out) -> (dQ, dK, dV)
+PyObject* window_attn_bwd(PyObject* const* a, Py_ssize_t n) {
+    if (n != 13) Py_RETURN_NONE;
+    bool ok = true;
+    double scale;
+    const Tensor *Q = cuda_tensor(a[0], ok), *K = cuda_tensor(a[1], ok), *V = cuda_tensor(a[2], ok), *O = cuda_tensor(a[3], ok), *lse = cuda_tensor(a[4], ok);
+    const Tensor *dO = cuda_tensor(a[5], ok), *len = tensor(a[9], ok), *ws = tensor(a[11], ok);
+    const int window = integer(a[6], ok), sinks = integer(a[7], ok), path = integer(a[10], ok);
+    psk_window_shape s;
+    if (!ok || !number(a[8], scale) || !window_shape(*Q, *K, V, len, window, sinks, scale, path, &s) || !bytes_ok(*Q, ws)) Py_RETURN_NONE;
+    if (!on_device_of(*Q, O) || !same_layout(*Q, O) || !on_device_of(*Q, dO) || !same_layout(*Q, dO)) Py_RETURN_NONE;
+    if (!on_device_of(*Q, lse) || lse->scalar_type() != at::kFloat || !lse->is_contiguous() || lse->numel() != (int64_t)s.B * s.H * s.n) Py_RETURN_NONE;
+    c10::cuda::CUDAGuard guard(Q->device());
+    Tensor g[3];
+    if (a[12] == Py_None) {
+        for (int i = 0; i < 3; ++i) g[i] = empty_as(i == 0 ? *Q : *K);
+    } else {
+        if (!PyTuple_Check(a[12]) || PyTuple_GET_SIZE(a[12]) != 3) Py_RETURN_NONE;
+        for (int i = 0; i < 3; ++i) {
+            const Tensor* t = tensor(PyTuple_GET_ITEM(a[12], i), ok);
+            if (!ok || t == nullptr || !on_device_of(*Q, t) || !same_layout(i == 0 ? *Q : *K, t)) Py_RETURN_NONE;
+            g[i] = *t;
+        }
+    }
+    Scratch w;
+    w.take(ws, api.window_bytes(&s, 1), 0, *Q);
+    int st;
+    void* cs = stream();
+    PSK_NO_GIL(st, api.window_bwd(&s, ptr(Q), ptr(K), ptr(V), (const int32_t*)ptr(len), ptr(O), (const float*)ptr(lse), ptr(dO), g[0].data_ptr(),
+                                  g[1].data_ptr(), g[2].data_ptr(), w.p, w.n, cs));
+    if (st != 0) return status_of(st);
+    PyObject* t = PyTuple_New(3);
+    for (int i = 0; i < 3; ++i) PyTuple_SET_ITEM(t, i, THPVariable_Wrap(std::move(g[i])));
+    return t;
+}
+
+// Kc, Vc: contiguous [B, Hkv, sinks + window, h]
+bool cache_ok(const Tensor& x, const Tensor* c, int64_t B, int64_t Hkv, int window, int sinks, int64_t h) {
+    return on_device_of(x, c) && c->scalar_type() == x.scalar_type() && c->dim() == 4 && c->is_contiguous() && c->size(0) == B && c->size(1) == Hkv &&
+           c->size(2) == (int64_t)window + sinks && c->size(3) == h;
+}
+
+// (K, V, Kc, Vc, window, sinks, lengths) -> True
+PyObject* window_cache_fill(PyObject* const* a, Py_ssize_t n) {
+    if (n != 7) Py_RETURN_NONE;
+    bool ok = true;
+    const Tensor *K = cuda_tensor(a[0], ok), *V = cuda_tensor(a[1], ok), *Kc = cuda_tensor(a[2], ok), *Vc = cuda_tensor(a[3], ok), *len = tensor(a[6], ok);
+    const int window = integer(a[4], ok), sinks = integer(a[5], ok);
+    psk_window_shape s;
+    if (!ok || !window_shape(*K, *K, V, len, window, sinks, 1.0, PSK_PATH_AUTO, &s)) Py_RETURN_NONE;
+    for (const Tensor* c : {Kc, Vc}) if (!cache_ok(*K, c, s.B, s.Hkv, window, sinks, s.h)) Py_RETURN_NONE;
+    c10::cuda::CUDAGuard guard(K->device());
+    int st;
+    void* cs = stream();
+    PSK_NO_GIL(st, api.window_fill(&s, ptr(K), ptr(V), (const int32_t*)ptr(len), ptr(Kc), ptr(Vc), cs));
+    if (st != 0) return status_of(st);
+    Py_RETURN_TRUE;
+}
+
+// (q, k, v, Kc, Vc, positions, window, sinks, scale, out) -> o
+PyObject* window_decode_step(PyObject* const* a, Py_ssize_t n) {
+    if (n != 10) Py_RETURN_NONE;
+    bool ok = true;
+    double scale;
+    const Tensor *q = cuda_tensor(a[0], ok), *k = cuda_tensor(a[1], ok), *v = cuda_tensor(a[2], ok), *Kc = cuda_tensor(a[3], ok), *Vc = cuda_tensor(a[4], ok);
+    const Tensor *pos = cuda_tensor(a[5], ok), *out = tensor(a[9], ok);
+    const int window = integer(a[6], ok), sinks = integer(a[7], ok);
+    if (!ok || !number(a[8], scale) || !storage_type(*q) || q->dim() != 3 || k->dim() != 3 || !q->is_contiguous() || !k->is_contiguous()) Py_RETURN_NONE;
+    if (k->scalar_type() != q->scalar_type() || !same_layout(*k, v) || !on_device_of(*q, k) || !on_device_of(*q, v)) Py_RETURN_NONE;
+    const int64_t B = q->size(0), H = q->size(1), Hkv = k->size(1), h = q->size(2);
+    if (B > INT32_MAX || H > INT32_MAX || Hkv > INT32_MAX || h > INT32_MAX || k->size(0) != B || k->size(2) != h) Py_RETURN_NONE;
+    for (const Tensor* c : {Kc, Vc}) if (!cache_ok(*q, c, B, Hkv, window, sinks, h)) Py_RETURN_NONE;
+    if (!on_device_of(*q, pos) || pos->scalar_type() != at::kInt || pos->dim() != 1 || pos->size(0) != B || !pos->is_contiguous()) Py_RETURN_NONE;
+    if (out != nullptr && (!on_device_of(*q, out) || !same_layout(*q, out))) Py_RETURN_NONE;
+    const psk_window_shape s{(int32_t)B, (int32_t)H, (int32_t)Hkv, 1, (int32_t)h, window, sinks, dtype_of(*q), PSK_PATH_AUTO, (float)scale, 0, 0, 0, 0, 0, 0};
+    c10::cuda::CUDAGuard guard(q->device());
+    Tensor o = out != nullptr ? *out : empty(q->sizes(), q->scalar_type(), *q);
+    int st;
+    void* cs = stream();
+    PSK_NO_GIL(st, api.window_step(&s, ptr(q), ptr(k), ptr(v), (const int32_t*)ptr(pos), ptr(Kc), ptr(Vc), o.data_ptr(), cs));
+    if (st != 0) return status_of(st);
+    return THPVariable_Wrap(std::move(o));
+}
+
 // init(addresses): the C ABI's entry points in the order of `Api`.
 PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (n != (Py_ssize_t)(sizeof(Api) / sizeof(void*))) { PyErr_SetString(PyExc_ValueError, "wrong number of entry points"); return nullptr; }
@@ -273,7 +493,8 @@ PyObject* guarded(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 #define PSK_M(f) {#f, (PyCFunction)(void (*)(void))guarded<f>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"init", (PyCFunction)(void (*)(void))init, METH_FASTCALL, nullptr}, PSK_M(attn_fwd), PSK_M(attn_bwd), PSK_M(decode_step), PSK_M(lt_multiply),
-                         PSK_M(learned_fwd), PSK_M(learned_bwd), {nullptr, nullptr, 0, nullptr}};
+                         PSK_M(learned_fwd), PSK_M(learned_bwd), PSK_M(layer_norm_fwd), PSK_M(layer_norm_bwd), PSK_M(window_attn_fwd),
+                         PSK_M(window_attn_bwd), PSK_M(window_cache_fill), PSK_M(window_decode_step), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_psk_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,503 @@
+// Layer normalisation of rows (Section 2.1: queries and keys come normalised to the attention), forward and backward.
+//   y = (x - mean) rstd gain + bias,   mean = sum(x) / C,   rstd = 1 / sqrt(sum((x - mean)^2) / C + eps)
+//   with a = dy gain,  xhat = (x - mean) rstd:
+//   dx = rstd (a - sum(a) / C - xhat sum(a xhat) / C),   dgain = sum over rows of dy xhat,   dbias = sum over rows of dy
+// Bound: memory.  A row is read once and stays in registers; the backward forms mean and rstd again from the x that it
+// reads anyway, so that nothing but x is kept from the forward (for rows of 64 in bf16 two stored floats would be 6 % of
+// the forward's bytes).  All sums in fp32, the variance from the deviations (two passes over registers).
+// A row belongs to G = 8, 16 or 32 lanes of a warp, or to a CTA; which, by how many 16-byte accesses it has (a lane keeps up to 32
+// values).  Rows whose address or stride is not a multiple of 16 bytes are read value by value.
+#include "psk_internal.cuh"
+
+#include <math.h>
+
+namespace psk {
+namespace {
+
+typedef __nv_bfloat16 bf16;
+constexpr int kNormThreads = 256, kNormWarps = kNormThreads / 32, kNormMaxCols = 8192;
+
+// x / d for 0 <= x < 2^31, 0 < d < 2^31 without a division: multiplication by ceil(2^(31 + s) / d), 2^s >= d
+// (the error of the reciprocal times x stays below 1/d).
+struct FastDiv {
+    uint32_t d, mul, shift;
+    void set(uint32_t v) {
+        d = v;
+        shift = 0;
+        while ((1ull << shift) < v) ++shift;
+        mul = v == 1 ? 0 : (uint32_t)(((1ull << (31 + shift)) + v - 1) / v);
+    }
+    __device__ __forceinline__ uint32_t div(uint32_t x) const { return mul == 0 ? x : __umulhi(x, mul) >> (shift - 1); }
+};
+
+struct NormArgs {
+    const void *x, *y;                // y: dY (backward only)
+    void* z;                          // Y or dX
+    const float *gain, *bias;
+    float *dgain, *dbias, *partial;   // partial [gridDim.x][2][cols], unless there is one CTA
+    uint32_t rows;
+    int cols;
+    float eps, over_cols;
+    FastDiv n1, n2;
+    int64_t xs[3], ys[3], zs[3];
+};
+
+__device__ __forceinline__ int64_t row_offset(const NormArgs& a, const int64_t (&s)[3], uint32_t r) {
+    const uint32_t q = a.n2.div(r), i2 = r - q * a.n2.d, i0 = a.n1.div(q), i1 = q - i0 * a.n1.d;
+    return (int64_t)i0 * s[0] + (int64_t)i1 * s[1] + (int64_t)i2 * s[2];
+}
+
+// V values at p: 16 bytes, or one value
+template <typename T, int V> struct Pack;
+template <> struct Pack<float, 4> {
+    float4 v;
+    __device__ __forceinline__ void load(const float* p) { v = *reinterpret_cast<const float4*>(p); }
+    __device__ __forceinline__ void zero() { v = make_float4(0.f, 0.f, 0.f, 0.f); }
+    __device__ __forceinline__ void get(float* f) const { f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w; }
+    __device__ __forceinline__ static void store(float* p, const float* f) { *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]); }
+};
+template <> struct Pack<bf16, 8> {
+    uint4 v;
+    __device__ __forceinline__ void load(const bf16* p) { v = *reinterpret_cast<const uint4*>(p); }
+    __device__ __forceinline__ void zero() { v = make_uint4(0, 0, 0, 0); }
+    __device__ __forceinline__ void get(float* f) const {
+        const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(u[i] << 16); f[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
+    }
+    __device__ __forceinline__ static void store(bf16* p, const float* f) {
+        uint32_t u[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(u[i]) : "f"(f[2 * i + 1]), "f"(f[2 * i]));
+        *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
+    }
+};
+template <typename T> struct Pack<T, 1> {
+    T v;
+    __device__ __forceinline__ void load(const T* p) { v = *p; }
+    __device__ __forceinline__ void zero() { stf(&v, 0.f); }
+    __device__ __forceinline__ void get(float* f) const { f[0] = ldf(&v); }
+    __device__ __forceinline__ static void store(T* p, const float* f) { stf(p, f[0]); }
+};
+
+// Sums of N values over the lanes of a row, in every lane.  `red`: shared memory for the rows of a whole CTA; callers alternate
+// between two of them, so that one barrier per sum is enough.
+template <int G, int N>
+__device__ __forceinline__ void row_sums(float (&s)[N], float (*red)[kNormWarps]) {
+    constexpr int W = G < 32 ? G : 32;
+#pragma unroll
+    for (int o = W / 2; o > 0; o >>= 1)
+#pragma unroll
+        for (int i = 0; i < N; ++i) s[i] += __shfl_xor_sync(0xffffffffu, s[i], o);
+    if constexpr (G > 32) {
+        if (threadIdx.x % 32 == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) red[i][threadIdx.x / 32] = s[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            s[i] = 0.f;
+#pragma unroll
+            for (int w = 0; w < kNormWarps; ++w) s[i] += red[i][w];
+        }
+    }
+}
+
+// s / cols: the product with the reciprocal, and its remainder (a row of one repeated value has that value as its mean)
+__device__ __forceinline__ float over_cols(const NormArgs& a, float s) {
+    const float m = s * a.over_cols;
+    return fmaf(fmaf(-m, (float)a.cols, s), a.over_cols, m);
+}
+
+// A row's lanes, and what they hold: accesses l, l + G, ... of V values each.
+template <int V, int NV, int G> struct RowMap {
+    static constexpr int kRowsPerCta = kNormThreads / G, kValues = V * NV;
+    static constexpr int kUnroll = NV == 1 ? (G < 32 ? 4 : 2) : 1;        // rows in flight per lane
+};
+
+template <typename T, int V, int NV, int G>
+__global__ void __launch_bounds__(kNormThreads)
+norm_fwd_kernel(const __grid_constant__ NormArgs a) {
+    using M = RowMap<V, NV, G>;
+    constexpr int U = M::kUnroll;
+    __shared__ float red[2][1][kNormWarps];
+    pdl_sync();
+    const int l = threadIdx.x % G, group = threadIdx.x / G, nvec = a.cols / V;
+    float gain[M::kValues], bias[M::kValues];
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int vec = l + k * G, c = vec * V + i;
+            gain[k * V + i] = (vec < nvec && a.gain != nullptr) ? a.gain[c] : 1.f;
+            bias[k * V + i] = (vec < nvec && a.bias != nullptr) ? a.bias[c] : 0.f;
+        }
+    const uint64_t step = (uint64_t)gridDim.x * M::kRowsPerCta;
+    // (the loop's bound is the same for all lanes of a CTA: rows beyond the last are computed as zeros and not stored)
+    for (uint64_t r0 = (uint64_t)blockIdx.x * M::kRowsPerCta; r0 < a.rows; r0 += step * U) {
+        Pack<T, V> x[U][NV];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint64_t r = r0 + u * step + group;
+            const T* row = (const T*)a.x + (r < a.rows ? row_offset(a, a.xs, (uint32_t)r) : 0);
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                const int vec = l + k * G;
+                if (r < a.rows && vec < nvec) x[u][k].load(row + vec * V); else x[u][k].zero();
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint64_t r = r0 + u * step + group;
+            float f[M::kValues], s[1] = {0.f}, q[1] = {0.f};
+#pragma unroll
+            for (int k = 0; k < NV; ++k) x[u][k].get(f + k * V);
+#pragma unroll
+            for (int i = 0; i < M::kValues; ++i) s[0] += f[i];
+            row_sums<G>(s, red[0]);
+            const float mean = over_cols(a, s[0]);
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+                if (l + k * G < nvec)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) { f[k * V + i] -= mean; q[0] = fmaf(f[k * V + i], f[k * V + i], q[0]); }
+            row_sums<G>(q, red[1]);
+            const float rstd = 1.f / sqrtf(q[0] * a.over_cols + a.eps);
+            if (r < a.rows) {
+                T* row = (T*)a.z + row_offset(a, a.zs, (uint32_t)r);
+#pragma unroll
+                for (int k = 0; k < NV; ++k) {
+                    const int vec = l + k * G;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) f[k * V + i] = fmaf(f[k * V + i] * rstd, gain[k * V + i], bias[k * V + i]);
+                    if (vec < nvec) Pack<T, V>::store(row + vec * V, f + k * V);
+                }
+            }
+        }
+    }
+}
+
+template <typename T, int V, int NV, int G>
+__global__ void __launch_bounds__(kNormThreads)
+norm_bwd_kernel(const __grid_constant__ NormArgs a) {
+    using M = RowMap<V, NV, G>;
+    constexpr int U = M::kUnroll > 2 ? 2 : M::kUnroll;
+    __shared__ float red1[1][kNormWarps], red2[3][kNormWarps];
+    extern __shared__ float sums[];                                       // [2][cols]
+    pdl_sync();
+    const int l = threadIdx.x % G, group = threadIdx.x / G, nvec = a.cols / V;
+    float dg[M::kValues], db[M::kValues];
+#pragma unroll
+    for (int i = 0; i < M::kValues; ++i) dg[i] = db[i] = 0.f;
+    // the gain stays in registers where a lane has few values; otherwise it is read again for every row (from L1)
+    constexpr bool kKeep = M::kValues <= 16;
+    float gain[kKeep ? M::kValues : 1];
+    if constexpr (kKeep)
+#pragma unroll
+        for (int i = 0; i < M::kValues; ++i) {
+            const int vec = l + i / V * G;
+            gain[i] = (vec < nvec && a.gain != nullptr) ? a.gain[vec * V + i % V] : 1.f;
+        }
+    const uint64_t step = (uint64_t)gridDim.x * M::kRowsPerCta;
+    for (uint64_t r0 = (uint64_t)blockIdx.x * M::kRowsPerCta; r0 < a.rows; r0 += step * U) {
+        Pack<T, V> x[U][NV], y[U][NV];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint64_t r = r0 + u * step + group;
+            const T* xrow = (const T*)a.x + (r < a.rows ? row_offset(a, a.xs, (uint32_t)r) : 0);
+            const T* yrow = (const T*)a.y + (r < a.rows ? row_offset(a, a.ys, (uint32_t)r) : 0);
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                const int vec = l + k * G;
+                if (r < a.rows && vec < nvec) { x[u][k].load(xrow + vec * V); y[u][k].load(yrow + vec * V); }
+                else { x[u][k].zero(); y[u][k].zero(); }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint64_t r = r0 + u * step + group;
+            float s[1] = {0.f};
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                float f[V];
+                x[u][k].get(f);
+#pragma unroll
+                for (int i = 0; i < V; ++i) s[0] += f[i];
+            }
+            row_sums<G>(s, red1);
+            const float mean = over_cols(a, s[0]);
+            // sums of the squared deviations, of a = dy gain, and of a times the deviation
+            float t[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                const int vec = l + k * G;
+                float f[V], d[V];
+                x[u][k].get(f);
+                y[u][k].get(d);
+                if (vec < nvec)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const float dev = f[i] - mean;
+                        const float ag = d[i] * (kKeep ? gain[kKeep ? k * V + i : 0] : (a.gain != nullptr ? a.gain[vec * V + i] : 1.f));
+                        t[0] = fmaf(dev, dev, t[0]);
+                        t[1] += ag;
+                        t[2] = fmaf(ag, dev, t[2]);
+                    }
+            }
+            row_sums<G>(t, red2);
+            const float rstd = 1.f / sqrtf(t[0] * a.over_cols + a.eps);
+            const float m1 = t[1] * a.over_cols, m2 = t[2] * a.over_cols * rstd;
+            if (r < a.rows) {
+                T* row = (T*)a.z + row_offset(a, a.zs, (uint32_t)r);
+#pragma unroll
+                for (int k = 0; k < NV; ++k) {
+                    const int vec = l + k * G;
+                    float f[V], d[V];
+                    x[u][k].get(f);
+                    y[u][k].get(d);
+                    if (vec < nvec) {
+#pragma unroll
+                        for (int i = 0; i < V; ++i) {
+                            const float xhat = (f[i] - mean) * rstd;
+                            const float ag = d[i] * (kKeep ? gain[kKeep ? k * V + i : 0] : (a.gain != nullptr ? a.gain[vec * V + i] : 1.f));
+                            dg[k * V + i] = fmaf(d[i], xhat, dg[k * V + i]);
+                            db[k * V + i] += d[i];
+                            f[i] = rstd * (ag - m1 - xhat * m2);
+                        }
+                        Pack<T, V>::store(row + vec * V, f);
+                    }
+                }
+            }
+        }
+    }
+    if (a.dgain == nullptr && a.dbias == nullptr) return;
+    // this CTA's sums over its rows: the rows side by side in a warp first, then warp after warp (a fixed order)
+#pragma unroll
+    for (int o = G; o < 32; o <<= 1)
+#pragma unroll
+        for (int i = 0; i < M::kValues; ++i) {
+            dg[i] += __shfl_xor_sync(0xffffffffu, dg[i], o);
+            db[i] += __shfl_xor_sync(0xffffffffu, db[i], o);
+        }
+    constexpr int kTurns = G > 32 ? 1 : kNormWarps;
+    const bool first_rows = G > 32 || threadIdx.x % 32 < G;
+    for (int w = 0; w < kTurns; ++w) {
+        if (first_rows && (G > 32 || (int)threadIdx.x / 32 == w))
+#pragma unroll
+            for (int i = 0; i < M::kValues; ++i) {
+                const int vec = l + i / V * G, c = vec * V + i % V;
+                if (vec < nvec) {
+                    sums[c] = (w > 0 ? sums[c] : 0.f) + dg[i];
+                    sums[a.cols + c] = (w > 0 ? sums[a.cols + c] : 0.f) + db[i];
+                }
+            }
+        __syncthreads();
+    }
+    for (int c = threadIdx.x; c < a.cols; c += kNormThreads) {
+        if (gridDim.x > 1) {
+            float* out = a.partial + (size_t)blockIdx.x * 2 * a.cols;
+            out[c] = sums[c];
+            out[a.cols + c] = sums[a.cols + c];
+        } else {
+            if (a.dgain != nullptr) a.dgain[c] = sums[c];
+            if (a.dbias != nullptr) a.dbias[c] = sums[a.cols + c];
+        }
+    }
+}
+
+// Sums of the CTAs' partial sums: 32 columns by 32 rows of threads.
+constexpr int kSumRows = 32;
+__global__ void __launch_bounds__(32 * kSumRows)
+norm_sum_kernel(const float* __restrict__ partial, int parts, int cols, float* __restrict__ dgain, float* __restrict__ dbias) {
+    __shared__ float s[kSumRows][33];
+    pdl_sync();
+    const int tx = threadIdx.x % 32, ty = threadIdx.x / 32, c = blockIdx.x * 32 + tx;
+    float t = 0.f;
+    if (c < 2 * cols)
+#pragma unroll 4
+        for (int p = ty; p < parts; p += kSumRows) t += partial[(size_t)p * 2 * cols + c];
+    s[ty][tx] = t;
+    __syncthreads();
+    // (transposed: a warp sums one column)
+    float u = s[tx][ty];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) u += __shfl_xor_sync(0xffffffffu, u, o);
+    const int oc = blockIdx.x * 32 + ty;
+    if (tx == 0 && oc < 2 * cols) {
+        if (oc < cols) { if (dgain != nullptr) dgain[oc] = u; }
+        else if (dbias != nullptr) dbias[oc - cols] = u;
+    }
+}
+
+// ---- host ----
+
+constexpr int kNormMaxCtas = 148 * 4;
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// extents and strides in the order of X's strides, so that neighbouring rows are read together
+struct Order { int32_t n[3]; int idx[3]; };
+Order order_of(const psk_norm_shape* sh) {
+    Order o{{sh->n0, sh->n1, sh->n2}, {0, 1, 2}};
+    for (int i = 0; i < 2; ++i)
+        for (int j = 0; j < 2 - i; ++j)
+            if (sh->xs[o.idx[j]] < sh->xs[o.idx[j + 1]] && o.n[j + 1] > 1) {
+                const int t = o.idx[j]; o.idx[j] = o.idx[j + 1]; o.idx[j + 1] = t;
+                const int32_t m = o.n[j]; o.n[j] = o.n[j + 1]; o.n[j + 1] = m;
+            }
+    return o;
+}
+
+// Rows that are written must not overlap: every extent steps over what lies inside it.
+bool rows_apart(const int32_t (&n)[3], const int64_t* s, int cols) {
+    int64_t end = cols;
+    bool used[3] = {false, false, false};
+    for (int k = 0; k < 3; ++k) {
+        int at = -1;
+        for (int i = 0; i < 3; ++i)
+            if (!used[i] && n[i] > 1 && (at < 0 || s[i] < s[at])) at = i;
+        if (at < 0) return true;
+        used[at] = true;
+        if (s[at] < end) return false;
+        end = s[at] * (n[at] - 1) + end;
+    }
+    return true;
+}
+
+int check_shape(const psk_norm_shape* sh, bool backward) {
+    if (sh == nullptr) return PSK_ERR_INVALID_ARG;
+    if (sh->dtype != PSK_F32 && sh->dtype != PSK_BF16) return PSK_ERR_INVALID_ARG;
+    if (!(sh->eps >= 0.f) || isinf(sh->eps)) return PSK_ERR_INVALID_ARG;
+    if (sh->n0 <= 0 || sh->n1 <= 0 || sh->n2 <= 0 || sh->cols <= 0) return PSK_ERR_SHAPE;
+    if (sh->cols > kNormMaxCols) return PSK_ERR_UNSUPPORTED;
+    if ((int64_t)sh->n0 * sh->n1 >= (int64_t)1 << 31 || (int64_t)sh->n0 * sh->n1 * sh->n2 >= (int64_t)1 << 31) return PSK_ERR_SHAPE;
+    const int32_t n[3] = {sh->n0, sh->n1, sh->n2};
+    for (int i = 0; i < 3; ++i)
+        if (n[i] > 1 && (sh->xs[i] < 0 || (backward && sh->ys[i] < 0))) return PSK_ERR_SHAPE;
+    return rows_apart(n, backward ? sh->zs : sh->ys, sh->cols) ? PSK_OK : PSK_ERR_SHAPE;
+}
+
+int grid_for(uint64_t rows, int rows_per_cta, int unroll) {
+    const uint64_t per = (uint64_t)rows_per_cta * unroll, want = (rows + per - 1) / per;
+    return (int)(want < (uint64_t)kNormMaxCtas ? want : (uint64_t)kNormMaxCtas);
+}
+
+template <typename T, int V, int NV, int G>
+cudaError_t launch(const NormArgs& a, bool backward, cudaStream_t s) {
+    using M = RowMap<V, NV, G>;
+    // (rows in flight only once every SM has its CTAs)
+    const uint64_t full = (uint64_t)kNormMaxCtas * M::kRowsPerCta;
+    const int grid = grid_for(a.rows, M::kRowsPerCta, a.rows > full ? 2 : 1);
+    if (!backward) {
+        prof_begin("norm_fwd_kernel", s);
+        launch_pdl(norm_fwd_kernel<T, V, NV, G>, dim3(grid), dim3(kNormThreads), 0, s, a);
+        prof_end(s);
+        return cudaGetLastError();
+    }
+    const bool params = a.dgain != nullptr || a.dbias != nullptr;
+    const size_t smem = params ? 2 * (size_t)a.cols * sizeof(float) : 0;
+    cudaError_t e = cudaFuncSetAttribute(norm_bwd_kernel<T, V, NV, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * kNormMaxCols * (int)sizeof(float));
+    if (e != cudaSuccess) return e;
+    prof_begin("norm_bwd_kernel", s);
+    launch_pdl(norm_bwd_kernel<T, V, NV, G>, dim3(grid), dim3(kNormThreads), smem, s, a);
+    prof_end(s);
+    if (params && grid > 1) {
+        prof_begin("norm_sum_kernel", s);
+        launch_pdl(norm_sum_kernel, dim3((2 * a.cols + 31) / 32), dim3(32 * kSumRows), 0, s, (const float*)a.partial, grid, a.cols, a.dgain, a.dbias);
+        prof_end(s);
+    }
+    return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t dispatch(const NormArgs& a, bool vec, bool backward, cudaStream_t s) {
+    constexpr int V = 16 / sizeof(T);
+    const int nvec = vec ? a.cols / V : a.cols;
+    if (!vec) {
+        if (nvec <= 32) return launch<T, 1, 1, 32>(a, backward, s);
+        if (nvec <= 128) return launch<T, 1, 4, 32>(a, backward, s);
+        if (nvec <= 512) return launch<T, 1, 16, 32>(a, backward, s);
+        if (nvec <= 1024) return launch<T, 1, 32, 32>(a, backward, s);
+        if (nvec <= 4096) return launch<T, 1, 16, kNormThreads>(a, backward, s);
+        return launch<T, 1, 32, kNormThreads>(a, backward, s);
+    }
+    if (nvec <= 8) return launch<T, V, 1, 8>(a, backward, s);
+    if (nvec <= 16) return launch<T, V, 1, 16>(a, backward, s);
+    if (nvec <= 32) return launch<T, V, 1, 32>(a, backward, s);
+    if (nvec <= 64) return launch<T, V, 2, 32>(a, backward, s);
+    if (nvec <= 96) return launch<T, V, 3, 32>(a, backward, s);
+    if (nvec <= 128) return launch<T, V, 4, 32>(a, backward, s);
+    if constexpr (V == 4) {
+        if (nvec <= 192) return launch<T, V, 6, 32>(a, backward, s);
+        if (nvec <= 256) return launch<T, V, 8, 32>(a, backward, s);
+        if (nvec <= 1024) return launch<T, V, 4, kNormThreads>(a, backward, s);
+        return launch<T, V, 8, kNormThreads>(a, backward, s);
+    } else {
+        if (nvec <= 256) return launch<T, V, 1, kNormThreads>(a, backward, s);
+        if (nvec <= 512) return launch<T, V, 2, kNormThreads>(a, backward, s);
+        return launch<T, V, 4, kNormThreads>(a, backward, s);
+    }
+}
+
+int run(const psk_norm_shape* sh, NormArgs& a, bool backward, cudaStream_t s) {
+    const Order o = order_of(sh);
+    a.rows = (uint32_t)sh->n0 * (uint32_t)sh->n1 * (uint32_t)sh->n2;
+    a.cols = sh->cols;
+    a.eps = sh->eps;
+    a.over_cols = 1.f / (float)sh->cols;
+    a.n1.set((uint32_t)o.n[1]);
+    a.n2.set((uint32_t)o.n[2]);
+    const int per = sh->dtype == PSK_F32 ? 4 : 8;
+    bool vec = sh->cols % per == 0;
+    for (const void* p : {a.x, a.y, (const void*)a.z}) vec = vec && aligned16(p);
+    const int64_t* in = sh->xs;
+    for (int i = 0; i < 3; ++i) {
+        const int k = o.idx[i];
+        a.xs[i] = in[k];
+        a.ys[i] = backward ? sh->ys[k] : 0;
+        a.zs[i] = backward ? sh->zs[k] : sh->ys[k];
+        if (o.n[i] > 1) vec = vec && a.xs[i] % per == 0 && a.ys[i] % per == 0 && a.zs[i] % per == 0;
+    }
+    const cudaError_t e = sh->dtype == PSK_F32 ? dispatch<float>(a, vec, backward, s) : dispatch<bf16>(a, vec, backward, s);
+    return e == cudaSuccess ? PSK_OK : PSK_ERR_CUDA;
+}
+
+}  // namespace
+}  // namespace psk
+
+using namespace psk;
+
+extern "C" {
+
+size_t psk_layer_norm_workspace_bytes(const psk_norm_shape* shape) {
+    if (check_shape(shape, true) != PSK_OK) return 0;
+    // partial sums of the most CTAs that a call has (a CTA has a row at least)
+    const uint64_t rows = (uint64_t)shape->n0 * shape->n1 * shape->n2;
+    const uint64_t ctas = rows < (uint64_t)kNormMaxCtas ? rows : (uint64_t)kNormMaxCtas;
+    return align_up((size_t)ctas * 2 * shape->cols * sizeof(float));
+}
+
+int psk_layer_norm_fwd(const psk_norm_shape* shape, const void* X, const float* gain, const float* bias, void* Y, void* stream) {
+    const int st = check_shape(shape, false);
+    if (st != PSK_OK) return st;
+    if (!X || !Y) return PSK_ERR_INVALID_ARG;
+    NormArgs a{};
+    a.x = X; a.z = Y; a.gain = gain; a.bias = bias;
+    return run(shape, a, false, (cudaStream_t)stream);
+}
+
+int psk_layer_norm_bwd(const psk_norm_shape* shape, const void* X, const float* gain, const void* dY, void* dX, float* dgain, float* dbias,
+                       void* workspace, size_t workspace_bytes, void* stream) {
+    const int st = check_shape(shape, true);
+    if (st != PSK_OK) return st;
+    if (!X || !dY || !dX) return PSK_ERR_INVALID_ARG;
+    if (dgain != nullptr || dbias != nullptr) {
+        if (!workspace || workspace_bytes < psk_layer_norm_workspace_bytes(shape) || (reinterpret_cast<uintptr_t>(workspace) & 15u)) return PSK_ERR_WORKSPACE;
+    }
+    NormArgs a{};
+    a.x = X; a.y = dY; a.z = dX; a.gain = gain; a.dgain = dgain; a.dbias = dbias;
+    a.partial = static_cast<float*>(workspace);
+    return run(shape, a, true, (cudaStream_t)stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,482 @@
+// Sliding-window softmax attention (exact attention next to the sketched one: Section 3.2 applies exact weights inside a block; here
+// a row sees the `window` rows up to its own, and the first `sinks` rows of its sequence) on the CUDA cores in
+// fp32 arithmetic, forward and backward; the cache that goes with it; the checks of all calls.
+#include "cc_gemm.cuh"
+#include "psk_window.cuh"
+
+#include <math.h>
+
+namespace psk {
+namespace win {
+namespace {
+
+using namespace cc;
+
+// ---------------------------------------------------------------------------
+// Forward and backward by 64 x 64 tiles, 64 threads (two warps) to a CTA, 8 x 8 of every product to a thread (cc_gemm.cuh).
+// Bound: fp32 FMA rate and the shared-memory loads behind it.  One tile of rows to a CTA, so that three to four CTAs share an
+// SM and one's loads hide behind another's products; a tile whose values are used up gives its place to the weights.
+// ---------------------------------------------------------------------------
+constexpr int kTile = 64, kThreads = 64;
+
+// 64 rows x 64 columns from row r0 into [64][kLd] fp32, zeros from row `end` on
+template <typename T>
+__device__ __forceinline__ void load_tile(float* dst, const T* src, int64_t stride, int r0, int end) {
+    constexpr int V = 16 / sizeof(T), PerRow = 64 / V;
+#pragma unroll 4
+    for (int e = threadIdx.x; e < kTile * PerRow; e += kThreads) {
+        const int r = e / PerRow, c = e % PerRow * V;
+        float* d = dst + r * kLd + c;
+        uint4 u = make_uint4(0, 0, 0, 0);
+        if (r0 + r < end) u = *reinterpret_cast<const uint4*>(src + (int64_t)(r0 + r) * stride + c);
+        if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<uint4*>(d) = u;
+        } else {
+            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) *reinterpret_cast<float2*>(d + 2 * i) = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+        }
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store4(T* p, float a, float b, float c, float d) {
+    if constexpr (sizeof(T) == 4) {
+        *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
+    } else {
+        uint32_t u, v;
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(u) : "f"(b), "f"(a));
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v) : "f"(d), "f"(c));
+        *reinterpret_cast<uint2*>(p) = make_uint2(u, v);
+    }
+}
+// Accumulator row i times f, as the thread's 8 of 64 columns; false if one of the row's 64 is not finite (the same in its 8 lanes).
+__device__ __forceinline__ bool row_out(const Acc& acc, int i, float f, float (&o)[8]) {
+    bool fine = true;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) { o[j] = acc.at(i, j) * f; fine = fine && finite(o[j]); }
+    const unsigned all = __ballot_sync(0xffffffffu, fine);
+    return (all >> (threadIdx.x % 32 / 8 * 8) & 0xffu) == 0xffu;
+}
+template <typename T>
+__device__ __forceinline__ void store_row(T* p, int cx, const float (&o)[8]) {
+    store4(p + 4 * cx, o[0], o[1], o[2], o[3]);
+    store4(p + 32 + 4 * cx, o[4], o[5], o[6], o[7]);
+}
+template <typename T>
+__device__ __forceinline__ void zero_rows(T* p, int64_t stride, int r0, int end) {
+    for (int e = threadIdx.x; e < kTile * 16; e += kThreads)
+        if (r0 + e / 16 < end) store4(p + (int64_t)(r0 + e / 16) * stride + e % 16 * 4, 0.f, 0.f, 0.f, 0.f);
+}
+
+struct Place { int b, h, row0, len; };
+__device__ __forceinline__ Place place_of(const WinArgs& a, int heads) {
+    const int tiles = (a.n + kTile - 1) / kTile, bh = blockIdx.x / tiles;
+    Place p;
+    p.b = bh / heads;
+    p.h = bh % heads;
+    p.row0 = (int)(blockIdx.x % tiles) * kTile;
+    p.len = length_of(a, p.b);
+    return p;
+}
+
+constexpr size_t kFwdSmem = 3 * kUnit * sizeof(float);
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+win_fwd_kernel(const __grid_constant__ WinArgs a) {
+    pdl_sync();
+    extern __shared__ float sm[];
+    __shared__ float s_al[kTile], s_inv[kTile];
+    __shared__ int s_bad[kTile];
+    float *sQ = sm, *sK = sm + kUnit, *sV = sm + 2 * kUnit, *sP = sK;         // the weights take the keys' place
+    const int tid = threadIdx.x, ry = tid / 8, cx = tid % 8;
+    const Place pl = place_of(a, a.H);
+    const T* Q = (const T*)a.Q + pl.b * a.qb + pl.h * a.qh;
+    const int64_t koff = pl.b * a.kb + pl.h / a.G * a.kh;
+    const T *K = (const T*)a.K + koff, *V = (const T*)a.V + koff;
+    T* O = (T*)a.out + pl.b * a.qb + pl.h * a.qh;
+    float* lse = a.lse + ((int64_t)pl.b * a.H + pl.h) * a.n;
+    const int row0 = pl.row0, len = pl.len, n_end = row0 + kTile < a.n ? row0 + kTile : a.n, end = row0 + kTile < len ? row0 + kTile : len;
+    // rows behind the sequence's end
+    zero_rows(O + (int64_t)(end > row0 ? end - row0 : 0) * a.qn, a.qn, row0, n_end - (end > row0 ? end - row0 : 0));
+    for (int r = (end > row0 ? end : row0) + tid; r < n_end; r += kThreads) lse[r] = neg_inf();
+    if (end <= row0) return;
+    load_tile(sQ, Q, a.qn, row0, end);
+    float m[8], l[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { m[i] = neg_inf(); l[i] = 0.f; }
+    Acc acc;
+    acc.zero();
+    const KeyTiles kt = key_tiles(row0, end - 1, a.window, a.sinks, kTile);
+    for (int x = 0; x < kt.count(); ++x) {
+        const int k0 = kt.at(x) * kTile;
+        __syncthreads();
+        load_tile(sK, K, a.kn, k0, len);
+        load_tile(sV, V, a.kn, k0, len);
+        __syncthreads();
+        float p[8][8];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            f2 d[4][8];
+            dot_half<kLd, kLd>(d, sQ, sK, 16, half, ry, cx);
+#pragma unroll
+            for (int i4 = 0; i4 < 4; ++i4) {
+                const int i = 4 * half + i4, row = row0 + ry + 8 * i;
+                float top = m[i];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float s = sum2(d[i4][j]) * a.c;
+                    p[i][j] = sees(row, k0 + cx + 8 * j, a.window, a.sinks) ? s : neg_inf();
+                    top = fmaxf(top, p[i][j]);
+                }
+#pragma unroll
+                for (int o = 1; o < 8; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                const float base = top == neg_inf() ? 0.f : top, alpha = exp2_approx(m[i] - base);
+                m[i] = top;
+                l[i] *= alpha;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) { p[i][j] = exp2_approx(p[i][j] - base); l[i] += p[i][j]; }
+                if (cx == 0) s_al[ry + 8 * i] = alpha;
+            }
+        }
+        __syncthreads();                                  // everyone has read the keys
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sP[(cx + 8 * j) * kLd + ry + 8 * i] = p[i][j];
+        __syncthreads();
+#pragma unroll
+        for (int p2 = 0; p2 < 4; ++p2) {
+            const f2 al = *reinterpret_cast<const f2*>(s_al + 8 * ry + 2 * p2);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) { acc.s[p2][q] = mul2(acc.s[p2][q], al); acc.x[p2][q] = mul2(acc.x[p2][q], al); }
+        }
+        outer_product(acc, sP, sV, kTile, kLd, ry, cx);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+        for (int o = 1; o < 8; o <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], o);
+        if (cx == 0) {
+            const int r = ry + 8 * i;
+            const float v = (m[i] + log2f(l[i])) * kLn2;
+            s_inv[r] = 1.f / l[i];
+            s_bad[r] = !finite(v);
+            if (row0 + r < end) lse[row0 + r] = v;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int r = out_row(ry, i);
+        float o[8];
+        const bool fine = row_out(acc, i, s_inv[r], o) && !s_bad[r];
+        __syncwarp();
+        if (row0 + r < end && fine) store_row(O + (int64_t)(row0 + r) * a.qn, cx, o);
+        if (cx == 0 && !fine) s_bad[r] = 1;
+    }
+    __syncthreads();
+    for (int r = tid / 32; row0 + r < end && r < kTile; r += kThreads / 32)
+        if (s_bad[r]) redo_out_row(Q + (int64_t)(row0 + r) * a.qn, K, V, a.kn, row0 + r, a.window, a.sinks, a.c, O + (int64_t)(row0 + r) * a.qn, lse + row0 + r);
+}
+
+constexpr size_t kDqSmem = 4 * kUnit * sizeof(float);
+
+// The gradient of 64 query rows; their D_i on the way, which the key side reads.
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+win_dq_kernel(const __grid_constant__ WinArgs a) {
+    pdl_sync();
+    extern __shared__ float sm[];
+    __shared__ float s_D[kTile], s_lse[kTile];
+    __shared__ int s_bad[kTile];
+    float *sQ = sm, *sG = sm + kUnit, *sK = sm + 2 * kUnit, *sV = sm + 3 * kUnit, *sP = sV;      // ds takes the values' place
+    const int tid = threadIdx.x, ry = tid / 8, cx = tid % 8;
+    const Place pl = place_of(a, a.H);
+    const int64_t qoff = pl.b * a.qb + pl.h * a.qh, koff = pl.b * a.kb + pl.h / a.G * a.kh, soff = ((int64_t)pl.b * a.H + pl.h) * a.n;
+    const T *Q = (const T*)a.Q + qoff, *dO = (const T*)a.dO + qoff, *O = (const T*)a.O + qoff, *K = (const T*)a.K + koff, *V = (const T*)a.V + koff;
+    T* dQ = (T*)a.dQ + qoff;
+    const int row0 = pl.row0, len = pl.len, n_end = row0 + kTile < a.n ? row0 + kTile : a.n, end = row0 + kTile < len ? row0 + kTile : len;
+    zero_rows(dQ + (int64_t)(end > row0 ? end - row0 : 0) * a.qn, a.qn, row0, n_end - (end > row0 ? end - row0 : 0));
+    for (int r = (end > row0 ? end : row0) + tid; r < n_end; r += kThreads) a.D[soff + r] = 0.f;
+    if (end <= row0) return;
+    load_tile(sQ, Q, a.qn, row0, end);
+    load_tile(sG, dO, a.qn, row0, end);
+    load_tile(sK, O, a.qn, row0, end);
+    __syncthreads();
+    {
+        float D = 0.f;
+#pragma unroll 8
+        for (int c = 0; c < 64; ++c) D = fmaf(sG[tid * kLd + c], sK[tid * kLd + c], D);
+        s_D[tid] = D;
+        s_lse[tid] = row0 + tid < end ? a.lse_in[soff + row0 + tid] * kLog2e : 0.f;
+        if (row0 + tid < end) a.D[soff + row0 + tid] = D;
+    }
+    Acc acc;
+    acc.zero();
+    const KeyTiles kt = key_tiles(row0, end - 1, a.window, a.sinks, kTile);
+    for (int x = 0; x < kt.count(); ++x) {
+        const int k0 = kt.at(x) * kTile;
+        __syncthreads();
+        load_tile(sK, K, a.kn, k0, len);
+        load_tile(sV, V, a.kn, k0, len);
+        __syncthreads();
+        float ds[8][8];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            f2 d[4][8];
+            dot_half<kLd, kLd>(d, sQ, sK, 16, half, ry, cx);
+#pragma unroll
+            for (int i4 = 0; i4 < 4; ++i4) {
+                const int i = 4 * half + i4, r = ry + 8 * i;
+                const float base = s_lse[r];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) ds[i][j] = sees(row0 + r, k0 + cx + 8 * j, a.window, a.sinks) ? exp2_approx(fmaf(sum2(d[i4][j]), a.c, -base)) : 0.f;
+            }
+            dot_half<kLd, kLd>(d, sG, sV, 16, half, ry, cx);
+#pragma unroll
+            for (int i4 = 0; i4 < 4; ++i4) {
+                const int i = 4 * half + i4, r = ry + 8 * i;
+                const float D = s_D[r];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) ds[i][j] = sees(row0 + r, k0 + cx + 8 * j, a.window, a.sinks) ? ds[i][j] * (sum2(d[i4][j]) - D) : 0.f;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sP[(cx + 8 * j) * kLd + ry + 8 * i] = ds[i][j];
+        __syncthreads();
+        outer_product(acc, sP, sK, kTile, kLd, ry, cx);
+    }
+    s_bad[tid] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int r = out_row(ry, i);
+        float o[8];
+        const bool fine = row_out(acc, i, a.scale, o);
+        if (row0 + r < end && fine) store_row(dQ + (int64_t)(row0 + r) * a.qn, cx, o);
+        if (cx == 0 && !fine) s_bad[r] = 1;
+    }
+    __syncthreads();
+    for (int r = tid / 32; row0 + r < end && r < kTile; r += kThreads / 32)
+        if (s_bad[r]) {
+            const int64_t at = (int64_t)(row0 + r) * a.qn;
+            redo_dq_row(Q + at, dO + at, K, V, a.kn, row0 + r, a.window, a.sinks, a.c, a.scale, a.lse_in[soff + row0 + r], s_D[r], dQ + at);
+        }
+}
+
+constexpr size_t kDkvSmem = 6 * kUnit * sizeof(float);
+
+// The gradients of 64 keys and values: sums over the query rows that see them, head by head of those that share them (a fixed order).
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+win_dkv_kernel(const __grid_constant__ WinArgs a) {
+    pdl_sync();
+    extern __shared__ float sm[];
+    __shared__ float s_D[kTile], s_lse[kTile];
+    __shared__ int s_bad[kTile];
+    float *sK = sm, *sV = sm + kUnit, *sQ = sm + 2 * kUnit, *sG = sm + 3 * kUnit, *sP = sm + 4 * kUnit, *sS = sm + 5 * kUnit;
+    const int tid = threadIdx.x, ry = tid / 8, cx = tid % 8;
+    const Place pl = place_of(a, a.Hkv);
+    const int64_t koff = pl.b * a.kb + pl.h * a.kh;
+    T *dK = (T*)a.dK + koff, *dV = (T*)a.dV + koff;
+    const int key0 = pl.row0, len = pl.len, n_end = key0 + kTile < a.n ? key0 + kTile : a.n, end = key0 + kTile < len ? key0 + kTile : len;
+    const int none = end > key0 ? end - key0 : 0;
+    zero_rows(dK + (int64_t)none * a.kn, a.kn, key0, n_end - none);
+    zero_rows(dV + (int64_t)none * a.kn, a.kn, key0, n_end - none);
+    if (end <= key0) return;
+    load_tile(sK, (const T*)a.K + koff, a.kn, key0, end);
+    load_tile(sV, (const T*)a.V + koff, a.kn, key0, end);
+    Acc ak, av;
+    ak.zero();
+    av.zero();
+    const int q_end = rows_end(key0, end - 1, a.window, a.sinks, len);
+    for (int g = 0; g < a.G; ++g) {
+        const int h = pl.h * a.G + g;
+        const int64_t qoff = pl.b * a.qb + h * a.qh, soff = ((int64_t)pl.b * a.H + h) * a.n;
+        const T *Q = (const T*)a.Q + qoff, *dO = (const T*)a.dO + qoff;
+        for (int i0 = key0; i0 < q_end; i0 += kTile) {
+            __syncthreads();
+            load_tile(sQ, Q, a.qn, i0, len);
+            load_tile(sG, dO, a.qn, i0, len);
+            s_D[tid] = i0 + tid < len ? a.D[soff + i0 + tid] : 0.f;
+            s_lse[tid] = i0 + tid < len ? a.lse_in[soff + i0 + tid] * kLog2e : 0.f;
+            __syncthreads();
+            // rows: queries; columns: keys
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                f2 d[4][8];
+                float p[4][8];
+                dot_half<kLd, kLd>(d, sQ, sK, 16, half, ry, cx);
+#pragma unroll
+                for (int i4 = 0; i4 < 4; ++i4) {
+                    const int r = ry + 8 * (4 * half + i4);
+                    const float base = s_lse[r];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const bool v = i0 + r < len && sees(i0 + r, key0 + cx + 8 * j, a.window, a.sinks);
+                        p[i4][j] = v ? exp2_approx(fmaf(sum2(d[i4][j]), a.c, -base)) : 0.f;
+                        sP[r * kLd + cx + 8 * j] = p[i4][j];
+                    }
+                }
+                dot_half<kLd, kLd>(d, sG, sV, 16, half, ry, cx);
+#pragma unroll
+                for (int i4 = 0; i4 < 4; ++i4) {
+                    const int r = ry + 8 * (4 * half + i4);
+                    const float D = s_D[r];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const bool v = i0 + r < len && sees(i0 + r, key0 + cx + 8 * j, a.window, a.sinks);
+                        sS[r * kLd + cx + 8 * j] = v ? p[i4][j] * (sum2(d[i4][j]) - D) : 0.f;
+                    }
+                }
+            }
+            __syncthreads();
+            outer_product(av, sP, sG, kTile, kLd, ry, cx);
+            outer_product(ak, sS, sQ, kTile, kLd, ry, cx);
+        }
+    }
+    s_bad[tid] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int r = out_row(ry, i);
+        float k[8], v[8];
+        const bool fk = row_out(ak, i, a.scale, k), fv = row_out(av, i, 1.f, v), fine = fk && fv;
+        if (key0 + r < end && fine) {
+            store_row(dK + (int64_t)(key0 + r) * a.kn, cx, k);
+            store_row(dV + (int64_t)(key0 + r) * a.kn, cx, v);
+        }
+        if (cx == 0 && !fine) s_bad[r] = 1;
+    }
+    __syncthreads();
+    for (int r = tid / 32; key0 + r < end && r < kTile; r += kThreads / 32)
+        if (s_bad[r]) redo_dkv_row<T>(a, pl.b, pl.h, key0 + r, len);
+}
+
+template <typename Kern>
+cudaError_t launch_rows(const char* name, Kern kern, size_t smem, unsigned grid, const WinArgs& a, cudaStream_t s) {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    prof_begin(name, s);
+    launch_pdl(kern, dim3(grid), dim3(kThreads), smem, s, a);
+    prof_end(s);
+    return cudaGetLastError();
+}
+template <typename T>
+cudaError_t cc_window_fwd(const WinArgs& a, cudaStream_t s) {
+    const unsigned tiles = (unsigned)((a.n + kTile - 1) / kTile);
+    return launch_rows("win_fwd_kernel", win_fwd_kernel<T>, kFwdSmem, tiles * a.B * a.H, a, s);
+}
+template <typename T>
+cudaError_t cc_window_bwd(const WinArgs& a, cudaStream_t s) {
+    const unsigned tiles = (unsigned)((a.n + kTile - 1) / kTile);
+    const cudaError_t e = launch_rows("win_dq_kernel", win_dq_kernel<T>, kDqSmem, tiles * a.B * a.H, a, s);
+    return e != cudaSuccess ? e : launch_rows("win_dkv_kernel", win_dkv_kernel<T>, kDkvSmem, tiles * a.B * a.Hkv, a, s);
+}
+
+}  // namespace
+
+// ---- host ----
+
+int check_common(const psk_window_shape* sh) {
+    if (sh == nullptr) return PSK_ERR_INVALID_ARG;
+    if (sh->dtype != PSK_F32 && sh->dtype != PSK_BF16) return PSK_ERR_INVALID_ARG;
+    if (sh->path < PSK_PATH_AUTO || sh->path > PSK_PATH_TENSOR_CORES) return PSK_ERR_INVALID_ARG;
+    if (!(sh->scale > 0.f) || isinf(sh->scale)) return PSK_ERR_INVALID_ARG;
+    if (sh->B <= 0 || sh->H <= 0 || sh->Hkv <= 0 || sh->H % sh->Hkv != 0) return PSK_ERR_SHAPE;
+    if (sh->window <= 0 || sh->sinks < 0) return PSK_ERR_SHAPE;
+    if ((int64_t)sh->B * sh->H >= (int64_t)1 << 31) return PSK_ERR_SHAPE;
+    return sh->h == 64 ? PSK_OK : PSK_ERR_UNSUPPORTED;
+}
+// [B,H,n,64] with these strides: rows that do not overlap, all on 16 bytes.  (The stride of an extent of 1 is not looked at.)
+static int check_strides(int64_t B, int64_t H, int64_t n, int64_t sb, int64_t sh, int64_t sn, int esz) {
+    const int64_t e[3] = {B, H, n}, s[3] = {sb, sh, sn};
+    bool used[3] = {false, false, false};
+    int64_t end = 64;
+    for (int k = 0; k < 3; ++k) {
+        int at = -1;
+        for (int i = 0; i < 3; ++i)
+            if (!used[i] && e[i] > 1 && (at < 0 || s[i] < s[at])) at = i;
+        if (at < 0) break;
+        used[at] = true;
+        if (s[at] < end || s[at] >= (int64_t)1 << 39) return PSK_ERR_SHAPE;
+        if (s[at] * esz % 16) return PSK_ERR_ALIGN;
+        end += s[at] * (e[at] - 1);
+    }
+    return PSK_OK;
+}
+int check_rows(const psk_window_shape* sh) {
+    int st = check_common(sh);
+    if (st != PSK_OK) return st;
+    if (sh->n <= 0 || (int64_t)sh->B * sh->H * sh->n >= (int64_t)1 << 31) return PSK_ERR_SHAPE;
+    if (sh->path == PSK_PATH_TENSOR_CORES) return PSK_ERR_UNSUPPORTED;
+    const int esz = sh->dtype == PSK_BF16 ? 2 : 4;
+    st = check_strides(sh->B, sh->H, sh->n, sh->q_stride_b, sh->q_stride_h, sh->q_stride_n, esz);
+    return st != PSK_OK ? st : check_strides(sh->B, sh->Hkv, sh->n, sh->kv_stride_b, sh->kv_stride_h, sh->kv_stride_n, esz);
+}
+WinArgs args_of(const psk_window_shape* sh) {
+    WinArgs a{};
+    a.B = sh->B; a.H = sh->H; a.Hkv = sh->Hkv; a.G = sh->H / sh->Hkv; a.n = sh->n;
+    a.window = sh->window; a.sinks = sh->sinks;
+    a.scale = sh->scale; a.c = sh->scale * kLog2e;
+    // (an extent of 1 gets a stride that a tensor map takes)
+    a.qb = sh->B > 1 ? sh->q_stride_b : 64; a.qh = sh->H > 1 ? sh->q_stride_h : 64; a.qn = sh->n > 1 ? sh->q_stride_n : 64;
+    a.kb = sh->B > 1 ? sh->kv_stride_b : 64; a.kh = sh->Hkv > 1 ? sh->kv_stride_h : 64; a.kn = sh->n > 1 ? sh->kv_stride_n : 64;
+    return a;
+}
+
+}  // namespace win
+}  // namespace psk
+
+using namespace psk;
+using namespace psk::win;
+
+extern "C" {
+
+size_t psk_window_workspace_bytes(const psk_window_shape* shape, int for_backward) {
+    if (check_rows(shape) != PSK_OK) return 0;
+    return kStatusBytes + (for_backward ? align_up((size_t)shape->B * shape->H * shape->n * sizeof(float)) : 0);
+}
+
+int psk_window_attn_fwd(const psk_window_shape* shape, const void* Q, const void* K, const void* V, const int32_t* lengths, void* O, float* lse,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+    const int st = check_rows(shape);
+    if (st != PSK_OK) return st;
+    if (!Q || !K || !V || !O || !lse) return PSK_ERR_INVALID_ARG;
+    for (const void* p : {Q, K, V, (const void*)O})
+        if (!aligned16(p)) return PSK_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(lse) | reinterpret_cast<uintptr_t>(lengths)) & 3u) return PSK_ERR_ALIGN;
+    if (!workspace || workspace_bytes < psk_window_workspace_bytes(shape, 0) || (reinterpret_cast<uintptr_t>(workspace) % kAlign)) return PSK_ERR_WORKSPACE;
+    cudaStream_t s = (cudaStream_t)stream;
+    WinArgs a = args_of(shape);
+    a.Q = Q; a.K = K; a.V = V; a.out = O; a.lse = lse; a.lengths = lengths;
+    cudaError_t e = cudaMemsetAsync(workspace, 0, sizeof(int), s);
+    if (e == cudaSuccess)
+        e = shape->dtype == PSK_F32 ? cc_window_fwd<float>(a, s) : cc_window_fwd<bf16>(a, s);
+    return e == cudaSuccess ? PSK_OK : PSK_ERR_CUDA;
+}
+
+int psk_window_attn_bwd(const psk_window_shape* shape, const void* Q, const void* K, const void* V, const int32_t* lengths, const void* O,
+                        const float* lse, const void* dO, void* dQ, void* dK, void* dV, void* workspace, size_t workspace_bytes, void* stream) {
+    const int st = check_rows(shape);
+    if (st != PSK_OK) return st;
+    if (!Q || !K || !V || !O || !lse || !dO || !dQ || !dK || !dV) return PSK_ERR_INVALID_ARG;
+    for (const void* p : {Q, K, V, O, dO, (const void*)dQ, (const void*)dK, (const void*)dV})
+        if (!aligned16(p)) return PSK_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(lse) | reinterpret_cast<uintptr_t>(lengths)) & 3u) return PSK_ERR_ALIGN;
+    if (!workspace || workspace_bytes < psk_window_workspace_bytes(shape, 1) || (reinterpret_cast<uintptr_t>(workspace) % kAlign)) return PSK_ERR_WORKSPACE;
+    cudaStream_t s = (cudaStream_t)stream;
+    WinArgs a = args_of(shape);
+    a.Q = Q; a.K = K; a.V = V; a.O = O; a.lse_in = lse; a.dO = dO; a.dQ = dQ; a.dK = dK; a.dV = dV; a.lengths = lengths;
+    a.D = reinterpret_cast<float*>(static_cast<char*>(workspace) + kStatusBytes);
+    cudaError_t e = cudaMemsetAsync(workspace, 0, sizeof(int), s);
+    if (e == cudaSuccess)
+        e = shape->dtype == PSK_F32 ? cc_window_bwd<float>(a, s) : cc_window_bwd<bf16>(a, s);
+    return e == cudaSuccess ? PSK_OK : PSK_ERR_CUDA;
+}
+
+}  // extern "C"

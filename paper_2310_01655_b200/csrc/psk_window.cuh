@@ -1,0 +1,154 @@
+// Sliding-window softmax attention: what its kernels share.
+//   row i of a sequence of length L (i < L) sees key j <=> j <= i and (i - j < window or j < sinks)
+//   s_ij = scale q_i . k_j,  lse_i = log sum_j exp(s_ij),  p_ij = exp(s_ij - lse_i),  o_i = sum_j p_ij v_j
+//   D_i = do_i . o_i,  ds_ij = p_ij (do_i . v_j - D_i),  dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij do_i
+// Scores are kept times log2(e), so that exponentials are powers of two.
+#pragma once
+
+#include "psk_internal.cuh"
+
+namespace psk {
+namespace win {
+
+typedef __nv_bfloat16 bf16;
+
+struct WinArgs {
+    const void *Q, *K, *V, *O, *dO;
+    void *out, *dQ, *dK, *dV;         // `out`: O of the forward
+    const float* lse_in;
+    float *lse, *D;                   // D: [B,H,n] scratch, written by the query side, read by the key side
+    const int32_t* lengths;           // [B] or null
+    int B, H, Hkv, G, n, window, sinks;
+    float scale, c;                   // c = scale log2(e)
+    int64_t qb, qh, qn, kb, kh, kn;   // element strides of the query-side and of the key-side tensors
+};
+
+__device__ __forceinline__ int length_of(const WinArgs& a, int b) {
+    if (a.lengths == nullptr) return a.n;
+    const int l = a.lengths[b];
+    return l < 0 ? 0 : (l > a.n ? a.n : l);
+}
+// (i - j and i - window + 1 do not overflow: 0 <= i, j < 2^31, window >= 1)
+__device__ __forceinline__ bool sees(int i, int j, int window, int sinks) { return j <= i && (i - j < window || j < sinks); }
+// the first key of row i's window
+__device__ __forceinline__ int window_start(int i, int window) { return i - window + 1 > 0 ? i - window + 1 : 0; }
+
+__device__ __forceinline__ float exp2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+__device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000); }
+__device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// ---- single rows by one warp, pair by pair ----
+// The tiled kernels multiply the weight 0 of a pair that the mask leaves out with the other row's values.  If an infinity or a NaN
+// stands there, it comes through as NaN.  So a result row that is not finite is formed again here from
+// the pairs that count alone (lane l holds columns 2 l and 2 l + 1).  Slow, and only there.
+template <typename T> __device__ __forceinline__ float2 ld2(const T* p) { return make_float2(ldf(p), ldf(p + 1)); }
+template <typename T> __device__ __forceinline__ void st2(T* p, float2 v) { stf(p, v.x); stf(p + 1, v.y); }
+__device__ __forceinline__ float dot2(float2 a, float2 b) { return warp_sum(fmaf(a.x, b.x, a.y * b.y)); }
+
+template <typename F>
+__device__ __forceinline__ void for_keys(int i, int window, int sinks, F&& f) {
+    const int lo = window_start(i, window), first = sinks < lo ? sinks : lo;
+    for (int j = 0; j < first; ++j) f(j);
+    for (int j = lo; j <= i; ++j) f(j);
+}
+
+// q, K, V, o: of row i and of its head
+template <typename T>
+__device__ __noinline__ void redo_out_row(const T* q, const T* K, const T* V, int64_t kn, int i, int window, int sinks, float c, T* o, float* lse) {
+    const int l2 = 2 * (threadIdx.x % 32);
+    const float2 qv = ld2(q + l2);
+    float m = neg_inf(), l = 0.f;
+    float2 acc = make_float2(0.f, 0.f);
+    for_keys(i, window, sinks, [&](int j) {
+        const float s = dot2(qv, ld2(K + j * kn + l2)) * c;
+        const float m2 = fmaxf(m, s);                     // (a NaN score: p is NaN, and so is the row)
+        const float base = m2 == neg_inf() ? 0.f : m2, alpha = exp2_approx(m - base), p = exp2_approx(s - base);
+        const float2 v = ld2(V + j * kn + l2);
+        acc.x = fmaf(acc.x, alpha, p * v.x);
+        acc.y = fmaf(acc.y, alpha, p * v.y);
+        l = fmaf(l, alpha, p);
+        m = m2;
+    });
+    st2(o + l2, make_float2(acc.x / l, acc.y / l));
+    if (l2 == 0) *lse = (m + log2f(l)) * kLn2;
+}
+
+template <typename T>
+__device__ __noinline__ void redo_dq_row(const T* q, const T* dO, const T* K, const T* V, int64_t kn, int i, int window, int sinks, float c, float scale,
+                                         float lse, float D, T* dq) {
+    const int l2 = 2 * (threadIdx.x % 32);
+    const float2 qv = ld2(q + l2), dv = ld2(dO + l2);
+    float2 acc = make_float2(0.f, 0.f);
+    for_keys(i, window, sinks, [&](int j) {
+        const float2 k = ld2(K + j * kn + l2);
+        const float p = exp2_approx(dot2(qv, k) * c - lse * kLog2e);
+        const float ds = p * (dot2(dv, ld2(V + j * kn + l2)) - D);
+        acc.x = fmaf(ds, k.x, acc.x);
+        acc.y = fmaf(ds, k.y, acc.y);
+    });
+    st2(dq + l2, make_float2(acc.x * scale, acc.y * scale));
+}
+
+// row j of key head hk of sequence b
+template <typename T>
+__device__ __noinline__ void redo_dkv_row(const WinArgs& a, int b, int hk, int j, int len) {
+    const int l2 = 2 * (threadIdx.x % 32);
+    const int64_t krow = b * a.kb + hk * a.kh + j * a.kn + l2;
+    const float2 k = ld2((const T*)a.K + krow), v = ld2((const T*)a.V + krow);
+    float2 dk = make_float2(0.f, 0.f), dv = dk;
+    const int64_t past = (int64_t)j + a.window;
+    const int end = (j < a.sinks || past > len) ? len : (int)past;
+    for (int g = 0; g < a.G; ++g) {
+        const int h = hk * a.G + g;
+        for (int i = j; i < end; ++i) {
+            const int64_t row = b * a.qb + h * a.qh + i * a.qn + l2, st = ((int64_t)b * a.H + h) * a.n + i;
+            const float2 q = ld2((const T*)a.Q + row), d = ld2((const T*)a.dO + row);
+            const float p = exp2_approx(dot2(q, k) * a.c - a.lse_in[st] * kLog2e);
+            const float ds = p * (dot2(d, v) - a.D[st]) * a.scale;
+            dv.x = fmaf(p, d.x, dv.x); dv.y = fmaf(p, d.y, dv.y);
+            dk.x = fmaf(ds, q.x, dk.x); dk.y = fmaf(ds, q.y, dk.y);
+        }
+    }
+    st2((T*)a.dK + krow, dk);
+    st2((T*)a.dV + krow, dv);
+}
+
+// The key tiles (of `tile` keys) that rows row0 .. row1 see any key of: [0, sink_tiles) and [band0, band1].
+struct KeyTiles {
+    int sink_tiles, band0, band1;
+    __device__ __forceinline__ int count() const { return sink_tiles + band1 - band0 + 1; }
+    __device__ __forceinline__ int at(int x) const { return x < sink_tiles ? x : band0 + x - sink_tiles; }
+};
+__device__ __forceinline__ KeyTiles key_tiles(int row0, int row1, int window, int sinks, int tile) {
+    KeyTiles k;
+    k.band0 = window_start(row0, window) / tile;
+    k.band1 = row1 / tile;
+    const int s = (int)(((int64_t)sinks + tile - 1) / tile);
+    k.sink_tiles = s < k.band0 ? s : k.band0;
+    return k;
+}
+// The last row (exclusive) that sees any of the keys key0 .. key1 of a sequence of `len`: later ones see none.
+__device__ __forceinline__ int rows_end(int key0, int key1, int window, int sinks, int len) {
+    const int64_t past = (int64_t)key1 + window;
+    return (key0 < sinks || past > len) ? len : (int)past;
+}
+
+// host: argument checks and what the kernels take (psk_window.cu)
+int check_common(const psk_window_shape* sh);         // all but n and the strides
+int check_rows(const psk_window_shape* sh);
+WinArgs args_of(const psk_window_shape* sh);
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+}  // namespace win
+}  // namespace psk

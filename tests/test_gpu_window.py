@@ -1,0 +1,324 @@
+"""Sliding-window attention, forward and backward, against the definition in 64 bits, element by element.
+
+Tolerances, from the roundings that the kernels make (u = 2^-24; e = 2^-8, half a step of bf16, or u for fp32 storage):
+* a score is off by (64 + 4) u scale sum|q||k| at most, so is its row's lse; with the exponential's 2^-22 a weight p is off by
+  p ep, ep = 2 * 68 u scale max_j sum|q||k_j| + 2^-21;
+* o = sum p v: p is rounded once as an operand (e, fp32: not), the sum over N rows in fp32 adds N u of its terms: error
+  (ep + e + N u) sum p|v|, plus the output's own rounding;
+* D = do.o from the stored o: |do|.(error of o) + 64 u |do|.|o|; do.v: 64 u |do|.|v|;
+* ds = p (do.v - D): |ds| (ep + e) + p (both errors); dq, dk, dv sum these times |k|, |q|, and (ep + e + N u) p times |do|."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2310_01655_b200 as psk
+from paper_2310_01655_b200 import binding
+from oracle import window as orc
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+E = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
+U = 2.0 ** -24
+
+
+def f64(x):
+    return x.detach().double().cpu().numpy()
+
+
+def make(dtype, B, H, Hkv, n, seed=0, spread=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    r = lambda h: torch.randn(B, h, n, 64, generator=g, device="cuda")
+    return tuple(x.to(DT[dtype]) for x in (r(H) * spread, r(Hkv) * spread, r(Hkv), r(H)))
+
+
+def within(name, got, ref, tol):
+    got = f64(got)
+    assert np.array_equal(np.isfinite(got), np.isfinite(ref)), name
+    fine = np.isfinite(ref)
+    # (a weight below 2^-126, fp32's smallest normal number, becomes 0: an error of at most 2^-126 for each, and a result is a sum of
+    # fewer than 2^16 of them times factors below 2^10)
+    off = np.abs(np.where(fine, got, 0) - np.where(fine, ref, 0))[fine] - np.broadcast_to(tol, ref.shape)[fine] - 2.0 ** -100
+    assert off.size == 0 or off.max() <= 0, "%s: off by %.3e more than allowed (%.3e)" % (name, off.max(), np.broadcast_to(tol, ref.shape)[fine].max())
+
+
+def check_heads(dtype, Q, K, V, dO, out, window, sinks, scale=None, lengths=None, heads=None):
+    """out: (O, lse, dQ, dK, dV) or (O, lse); whole groups of query heads that share a key head are looked at."""
+    B, H, n, _ = Q.shape
+    Hkv, G = K.shape[1], H // K.shape[1]
+    sc = 0.125 if scale is None else scale
+    e = E[dtype]
+    p_e = e if dtype == "bf16" else 0.0
+    for b, hk in (heads or {(0, 0), (B - 1, Hkv - 1)}):
+        L = None if lengths is None else int(lengths[b])
+        k, v = f64(K[b, hk]), f64(V[b, hk])
+        dk, dv, tk, tv = (np.zeros((n, 64)) for _ in range(4))
+        for h in range(hk * G, hk * G + G):
+            q = f64(Q[b, h])
+            M = orc.visible(n, window, sinks, L)
+            k0, v0, q0 = (np.where(np.isfinite(x), x, 0) for x in (k, v, q))
+            O, lse, P = orc.window_attention(q, k, v, window, sinks, sc, L)
+            S = np.where(M, np.abs(q0) @ np.abs(k0).T, 0) * sc
+            ep = 2 * 68 * U * S.max(1, keepdims=True) + 2.0 ** -21
+            N = M.sum(1, keepdims=True) + 64
+            t_o = (ep + p_e + N * U) * (P @ np.abs(v0)) + e * np.abs(O)
+            within("O[%d,%d]" % (b, h), out[0][b, h], O, t_o)
+            within("lse[%d,%d]" % (b, h), out[1][b, h], lse, (ep[:, 0] + N[:, 0] * U) + 4 * U * np.abs(np.where(np.isfinite(lse), lse, 0)))
+            if len(out) == 2:
+                continue
+            d = f64(dO[b, h])
+            d0 = np.where(np.isfinite(d), d, 0)
+            rq, rk, rv = orc.window_attention_backward(q, k, v, d, window, sinks, sc, L)
+            D = (d0 * O).sum(1, keepdims=True)
+            dp = np.where(M, d0 @ v0.T, 0)
+            eD = (np.abs(d0) * t_o).sum(1, keepdims=True) + 64 * U * (np.abs(d0) * np.abs(O)).sum(1, keepdims=True)
+            eds = np.abs(P * (dp - D)) * (ep + p_e + 4 * U) + P * (eD + 64 * U * np.where(M, np.abs(d0) @ np.abs(v0).T, 0))
+            N2 = (M.sum(0)[:, None] * G + 64) * U
+            ds = np.abs(P * (dp - D)) + eds
+            within("dQ[%d,%d]" % (b, h), out[2][b, h], rq, sc * (eds + N * U * ds) @ np.abs(k0) + (e + 2 * U) * np.abs(rq))
+            dk += rk
+            dv += rv
+            tk += sc * (eds.T @ np.abs(q0) + N2 * (ds.T @ np.abs(q0)))
+            tv += (P * (ep + p_e)).T @ np.abs(d0) + N2 * (P.T @ np.abs(d0))
+        if len(out) > 2:
+            within("dK[%d,%d]" % (b, hk), out[3][b, hk], dk, tk + (e + 2 * U) * (np.abs(dk) + tk))
+            within("dV[%d,%d]" % (b, hk), out[4][b, hk], dv, tv + (e + 2 * U) * (np.abs(dv) + tv))
+
+
+def run(Q, K, V, dO, window, sinks=0, **more):
+    ws = torch.empty(psk.binding.window_workspace_bytes(psk.binding.make_window_shape(Q, K, window, sinks), True), dtype=torch.uint8, device="cuda")
+    O, lse = psk.window_attn_fwd(Q, K, V, window, sinks, workspace=ws, **more)
+    assert psk.check(ws) == 0
+    grads = psk.window_attn_bwd(Q, K, V, O, lse, dO, window, sinks, workspace=ws, **more)
+    assert psk.check(ws) == 0
+    return (O, lse) + grads
+
+
+PATHS = [("f32", psk.PATH_AUTO), ("bf16", psk.PATH_AUTO), ("bf16", psk.PATH_CUDA_CORES)]
+
+
+@pytest.mark.parametrize("dtype,path", PATHS)
+@pytest.mark.parametrize("B,H,Hkv,n,window,sinks", [
+    (1, 1, 1, 1, 1, 0), (1, 1, 1, 1, 50, 3), (1, 2, 1, 2, 1, 0), (2, 2, 2, 5, 2, 1), (1, 1, 1, 63, 17, 0), (1, 1, 1, 64, 64, 0), (1, 3, 1, 65, 33, 2),
+    (2, 2, 2, 127, 200, 0), (1, 2, 2, 128, 128, 0), (1, 1, 1, 129, 1, 0), (1, 4, 2, 200, 1, 5), (1, 2, 2, 255, 63, 0), (1, 1, 1, 256, 64, 64),
+    (1, 1, 1, 257, 65, 1), (1, 2, 1, 300, 100, 130), (2, 4, 4, 320, 129, 4), (1, 8, 1, 385, 96, 7), (1, 1, 1, 385, 2**31 - 1, 0),
+    (1, 1, 1, 300, 20, 2**31 - 1), (1, 1, 1, 513, 127, 3), (1, 2, 2, 640, 128, 0), (1, 6, 2, 700, 260, 200), (1, 1, 1, 897, 256, 16)])
+def test_against_the_definition(dtype, path, B, H, Hkv, n, window, sinks):
+    Q, K, V, dO = make(dtype, B, H, Hkv, n, seed=n + window % 1000)
+    out = run(Q, K, V, dO, window, sinks, path=path)
+    check_heads(dtype, Q, K, V, dO, out, window, sinks)
+    for x, y in zip(out, run(Q, K, V, dO, window, sinks, path=path)):
+        assert torch.equal(x, y)                              # every sum in a fixed order
+
+
+@pytest.mark.parametrize("dtype,path", PATHS)
+@pytest.mark.parametrize("window,sinks", [(40, 0), (150, 5), (300, 140), (1000, 0)])
+def test_sequences_of_all_lengths(dtype, path, window, sinks):
+    n = 391
+    lengths = [n, 0, 1, 63, 64, 65, 127, 128, 129, 200, 256, 257, 390, -5, n + 9]
+    Q, K, V, dO = make(dtype, len(lengths), 2, 1, n, seed=window)
+    lens = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    out = run(Q, K, V, dO, window, sinks, path=path, lengths=lens)
+    for b, L in enumerate(lengths):
+        L = max(0, min(L, n))
+        assert (out[0][b, :, L:] == 0).all() and (out[1][b, :, L:] == float("-inf")).all()
+        assert all((x[b, :, L:] == 0).all() for x in out[2:])
+    check_heads(dtype, Q, K, V, dO, out, window, sinks, lengths=lens.tolist(), heads=[(b, 0) for b in range(len(lengths))])
+    # what stands behind a sequence's end does not count
+    for b, L in enumerate(lengths):
+        L = max(0, min(L, n))
+        for x in (Q, K, V, dO):
+            x[b, :, L:] = float("nan") if b % 2 else float("inf")
+    for x, y in zip(out, run(Q, K, V, dO, window, sinks, path=path, lengths=lens)):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype,path", PATHS)
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("window,sinks", [(70, 0), (200, 3), (2000, 0)])
+def test_masked_infinities_and_nans(dtype, path, bad, window, sinks):
+    """A row is not touched by what stands in rows that it does not see, not even where both lie in one tile."""
+    n = 450
+    Q, K, V, dO = make(dtype, 1, 2, 1, n, seed=17)
+    for s in (201, 330):
+        later, earlier = slice(s, None), slice(None, s)
+        Q2, K2, V2, d2 = (x.clone() for x in (Q, K, V, dO))
+        for x in (Q2, K2, V2, d2):
+            x[:, :, later] = bad
+        got = run(Q2, K2, V2, d2, window, sinks, path=path)
+        part = lambda x: x[:, :, earlier].contiguous()
+        assert torch.isfinite(got[0][:, :, earlier]).all() and torch.isfinite(got[2][:, :, earlier]).all()
+        check_heads(dtype, part(Q), part(K), part(V), part(dO), (part(got[0]), part(got[1])), window, sinks)
+        rq = orc.window_attention_backward(f64(Q[0, 1])[:s], f64(K[0, 0])[:s], f64(V[0, 0])[:s], f64(dO[0, 1])[:s], window, sinks)[0]
+        assert np.linalg.norm(f64(got[2][0, 1, earlier]) - rq) <= 4 * max(E[dtype], 1e-6) * np.linalg.norm(rq)
+        # keys behind the last bad query row: of earlier queries nothing counts
+        Q2, d2 = Q.clone(), dO.clone()
+        for x in (Q2, d2):
+            x[:, :, earlier] = bad
+        got = run(Q2, K, V, d2, window, sinks, path=path)
+        clean = run(Q, K, V, dO, window, sinks, path=path)
+        for x, y, name in zip(got[3:], clean[3:], ("dK", "dV")):
+            x, y = f64(x[:, :, later]), f64(y[:, :, later])
+            assert np.isfinite(x).all(), name
+            assert np.linalg.norm(x - y) <= 4 * max(E[dtype], 1e-6) * np.linalg.norm(y), name
+    # and a key too old to be seen
+    if window < n:
+        K2, V2 = K.clone(), V.clone()
+        K2[:, :, 100] = bad
+        V2[:, :, 100] = bad
+        got = run(Q, K2, V2, dO, window, sinks, path=path)
+        assert torch.isfinite(got[0][:, :, 100 + window:]).all() and torch.isfinite(got[2][:, :, 100 + window:]).all()
+        assert not torch.isfinite(got[0][:, :, 100:100 + window].float()).any(-1).any()
+
+
+@pytest.mark.parametrize("dtype,path", PATHS)
+def test_large_scores(dtype, path):
+    # weights that are one or nothing, scores in the hundreds, growing along the row so that the running maximum moves on
+    n, window = 300, 170
+    Q, K, V, dO = make(dtype, 1, 1, 1, n, seed=3, spread=4.0)
+    K = (K.float() * torch.linspace(0.2, 3.0, n, device="cuda")[None, None, :, None]).to(K.dtype)
+    out = run(Q, K, V, dO, window, 2, path=path)
+    check_heads(dtype, Q, K, V, dO, out, window, 2)
+    out = run(Q, K.flip(2).contiguous(), V, dO, window, 2, path=path)
+    check_heads(dtype, Q, K.flip(2), V, dO, out, window, 2)
+
+
+@pytest.mark.parametrize("dtype,path", PATHS)
+@pytest.mark.parametrize("scale", [1e-4, 0.3, 1.0])
+def test_scales(dtype, path, scale):
+    Q, K, V, dO = make(dtype, 1, 2, 2, 150, seed=4)
+    out = run(Q, K, V, dO, 70, 1, path=path, scale=scale)
+    check_heads(dtype, Q, K, V, dO, out, 70, 1, scale=scale)
+
+
+@pytest.mark.parametrize("dtype,path", PATHS)
+def test_inside_a_projection(dtype, path):
+    """[B, n, (H + 2 Hkv), 64] as a projection leaves it; queries and keys have strides of their own."""
+    B, n, H, Hkv, window, sinks = 2, 333, 4, 2, 90, 3
+    g = torch.Generator(device="cuda").manual_seed(6)
+    proj = torch.randn(B, n, H + 2 * Hkv, 64, generator=g, device="cuda").to(DT[dtype])
+    Q, K, V = (proj[:, :, a:b].transpose(1, 2) for a, b in ((0, H), (H, H + Hkv), (H + Hkv, H + 2 * Hkv)))
+    dO = torch.empty_strided(Q.shape, Q.stride(), dtype=Q.dtype, device="cuda")
+    dO.copy_(torch.randn(B, H, n, 64, generator=g, device="cuda"))
+    before = proj.clone()
+    out = run(Q, K, V, dO, window, sinks, path=path)
+    assert torch.equal(proj, before) and out[0].stride() == Q.stride() and out[3].stride() == K.stride()
+    dense = run(*(x.contiguous() for x in (Q, K, V, dO)), window, sinks, path=path)
+    for x, y in zip(out, dense):
+        assert torch.equal(x, y)
+    # outputs into a buffer of gradients of the projection: what lies between is left as it was
+    gp = torch.full_like(proj, 7.0)
+    views = tuple(gp[:, :, a:b].transpose(1, 2) for a, b in ((0, H), (H, H + Hkv), (H + Hkv, H + 2 * Hkv)))
+    psk.window_attn_bwd(Q, K, V, out[0], out[1], dO, window, sinks, path=path, out=views)
+    for x, y in zip(views, out[2:]):
+        assert torch.equal(x, y)
+    with pytest.raises(ValueError):
+        psk.window_attn_bwd(Q, K, V, out[0].contiguous(), out[1], dO, window, sinks, path=path)
+
+
+@pytest.mark.parametrize("dtype,path", PATHS)
+def test_rows_far_apart(dtype, path):
+    # element offsets that pass 32 bits
+    n, step = 140, 17_000_000
+    Q, K, V, dO = make(dtype, 1, 1, 1, n, seed=7)
+    big = torch.empty(n * step, dtype=Q.dtype, device="cuda")
+    far = lambda x, at: big.as_strided((1, 1, n, 64), (n * step, n * step, step, 1), at).copy_(x)
+    ref = run(Q, K, V, dO, 50, 2, path=path)
+    q, k, v, d = (far(x, 64 * i) for i, x in enumerate((Q, K, V, dO)))
+    outs = [big.as_strided((1, 1, n, 64), (n * step, n * step, step, 1), 64 * (4 + i)) for i in range(4)]
+    O, lse = psk.window_attn_fwd(q, k, v, 50, 2, path=path, out=outs[0])
+    grads = psk.window_attn_bwd(q, k, v, O, lse, d, 50, 2, path=path, out=tuple(outs[1:]))
+    for x, y in zip((O, lse) + tuple(grads), ref):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_graph_stream_and_ctypes(dtype, monkeypatch):
+    Q, K, V, dO = make(dtype, 2, 4, 2, 270, seed=8)
+    lens = torch.tensor([270, 111], dtype=torch.int32, device="cuda")
+
+    def step():
+        O, lse = psk.window_attn_fwd(Q, K, V, 100, 3, lengths=lens)
+        return (O, lse) + psk.window_attn_bwd(Q, K, V, O, lse, dO, 100, 3, lengths=lens)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for x, y in zip((Q, K, V, dO), make(dtype, 2, 4, 2, 270, seed=9)):
+        x.copy_(y)
+    lens.copy_(torch.tensor([33, 270]))
+    graph.replay()
+    torch.cuda.synchronize()
+    ref = step()
+    for x, y in zip(got, ref):
+        assert torch.equal(x, y)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = step()
+    side.synchronize()
+    monkeypatch.setattr(binding, "_fast", binding._NoNative())
+    for x, y, z in zip(ref, other, step()):
+        assert torch.equal(x, y) and torch.equal(x, z)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_two_streams_at_once(dtype):
+    sets = [make(dtype, 2, 3, 3, 600, seed=30 + i) for i in range(2)]
+    refs = [run(*s, 130, 2) for s in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    outs = [[], []]
+    for _ in range(5):
+        for i, (st, s) in enumerate(zip(streams, sets)):
+            with torch.cuda.stream(st):
+                O, lse = psk.window_attn_fwd(*s[:3], 130, 2)
+                outs[i].append((O, lse) + psk.window_attn_bwd(*s[:3], O, lse, s[3], 130, 2))
+    torch.cuda.synchronize()
+    for ref, got in zip(refs, outs):
+        for one in got:
+            for x, y in zip(ref, one):
+                assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gradients_are_differences(dtype):
+    """Along random directions: d/de sum(O . dO), O from the oracle's forward (64 bits) at the stored inputs."""
+    n, window, sinks = 90, 30, 2
+    Q, K, V, dO = make(dtype, 1, 1, 1, n, seed=10)
+    grads = run(Q, K, V, dO, window, sinks)[2:]
+    q, k, v, d = (f64(x[0, 0]) for x in (Q, K, V, dO))
+    g = np.random.default_rng(11)
+    f = lambda *a: (orc.window_attention(*a, window, sinks)[0] * d).sum()
+    for i, got in enumerate(grads):
+        D = f64(got[0, 0]) + np.linalg.norm(f64(got[0, 0])) / 80 * g.normal(size=(n, 64))       # (a direction that the gradient is not small along)
+        a = lambda s: f(*[x + s * 1e-5 * D if j == i else x for j, x in enumerate((q, k, v))])
+        diff = (a(1) - a(-1)) / 2e-5
+        # errors of the gradient's elements are at most 3 half steps (p or ds, the output, D) and of either sign
+        assert abs(diff - (f64(got[0, 0]) * D).sum()) <= 3 * max(E[dtype], 1e-6) * np.linalg.norm(f64(got[0, 0])) * np.linalg.norm(D)
+
+
+def test_refusals():
+    Q, K, V, dO = make("bf16", 2, 4, 2, 40)
+    lens = torch.tensor([40, 3], dtype=torch.int32, device="cuda")
+    O, lse = psk.window_attn_fwd(Q, K, V, 8)
+    for call in (lambda: psk.window_attn_fwd(Q, K, V[:, :, :39], 8), lambda: psk.window_attn_fwd(Q, K.float(), V.float(), 8),
+                 lambda: psk.window_attn_fwd(Q.half(), K.half(), V.half(), 8), lambda: psk.window_attn_fwd(Q, K, V, 8, lengths=lens.long()),
+                 lambda: psk.window_attn_fwd(Q, K, V, 8, lengths=lens[:1]), lambda: psk.window_attn_fwd(Q, K[:1], V[:1], 8),
+                 lambda: psk.window_attn_fwd(Q[0], K, V, 8), lambda: psk.window_attn_fwd(Q, K, V, 8, lse=lse.double()),
+                 lambda: psk.window_attn_fwd(Q, K, V, 8, out=O.float()), lambda: psk.window_attn_fwd(Q, K, V, 8, workspace=lse),
+                 lambda: psk.window_attn_bwd(Q, K, V, O, lse[:1], dO, 8), lambda: psk.window_attn_bwd(Q, K, V, O, lse, dO.float(), 8)):
+        with pytest.raises(ValueError):
+            call()
+    for call, code in ((lambda: psk.window_attn_fwd(Q, K, V, 0), -3), (lambda: psk.window_attn_fwd(Q, K, V, 8, -1), -3),
+                       (lambda: psk.window_attn_fwd(Q, K, V, 8, scale=0.0), -1), (lambda: psk.window_attn_fwd(Q[:, :3].contiguous(), K, V, 8), -3),
+                       (lambda: psk.window_attn_fwd(Q[..., :32].contiguous(), K[..., :32].contiguous(), V[..., :32].contiguous(), 8), -2),
+                       (lambda: psk.window_attn_fwd(Q.float(), K.float(), V.float(), 8, path=psk.PATH_TENSOR_CORES), -2),
+                       (lambda: psk.window_attn_fwd(Q[:, :1].expand(2, 4, 40, 64), K, V, 8), -3),
+                       (lambda: psk.window_attn_fwd(Q, K, V, 8, workspace=torch.empty(8, dtype=torch.uint8, device="cuda")), -5)):
+        with pytest.raises(psk.PskError) as e:
+            call()
+        assert e.value.code == code
+    with pytest.raises(RuntimeError):
+        psk.window_attn_fwd(Q, K.cpu(), V.cpu(), 8)
