@@ -302,8 +302,9 @@ int psk_layer_norm_bwd(const psk_norm_shape* shape, const void* X, const float* 
  *   workspace      DEVICE scratch, 256-byte aligned, >= psk_window_workspace_bytes(shape, for_backward) (0 for a bad
  *                  shape); its first word is the status that psk_check() reads
  * Query head h reads key head h / (H / Hkv); dK and dV are summed over the query heads that share one, in a fixed
- * order.  h = 64, any n >= 1, window >= 1, sinks >= 0, scale > 0.  CUDA cores, fp32 arithmetic.
- * The backward takes D_i = do_i . o_i from the stored O. */
+ * order.  h = 64, any n >= 1, window >= 1, sinks >= 0, scale > 0.  fp32 storage: CUDA cores, fp32 arithmetic.  bf16 storage: tensor
+ * cores with fp32 accumulation, weights and their gradients rounded to bf16 once as operands (PSK_PATH_CUDA_CORES: fp32
+ * arithmetic throughout).  The backward takes D_i = do_i . o_i from the stored O. */
 typedef struct {
     int32_t B, H, Hkv, n, h, window, sinks;
     int32_t dtype;              /* psk_dtype */

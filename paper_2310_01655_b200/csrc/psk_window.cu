@@ -85,6 +85,7 @@ template <typename T>
 __global__ void __launch_bounds__(kThreads)
 win_fwd_kernel(const __grid_constant__ WinArgs a) {
     pdl_sync();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0;
     extern __shared__ float sm[];
     __shared__ float s_al[kTile], s_inv[kTile];
     __shared__ int s_bad[kTile];
@@ -187,6 +188,7 @@ template <typename T>
 __global__ void __launch_bounds__(kThreads)
 win_dq_kernel(const __grid_constant__ WinArgs a) {
     pdl_sync();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0;
     extern __shared__ float sm[];
     __shared__ float s_D[kTile], s_lse[kTile];
     __shared__ int s_bad[kTile];
@@ -413,11 +415,12 @@ int check_rows(const psk_window_shape* sh) {
     int st = check_common(sh);
     if (st != PSK_OK) return st;
     if (sh->n <= 0 || (int64_t)sh->B * sh->H * sh->n >= (int64_t)1 << 31) return PSK_ERR_SHAPE;
-    if (sh->path == PSK_PATH_TENSOR_CORES) return PSK_ERR_UNSUPPORTED;
+    if (sh->path == PSK_PATH_TENSOR_CORES && sh->dtype != PSK_BF16) return PSK_ERR_UNSUPPORTED;
     const int esz = sh->dtype == PSK_BF16 ? 2 : 4;
     st = check_strides(sh->B, sh->H, sh->n, sh->q_stride_b, sh->q_stride_h, sh->q_stride_n, esz);
     return st != PSK_OK ? st : check_strides(sh->B, sh->Hkv, sh->n, sh->kv_stride_b, sh->kv_stride_h, sh->kv_stride_n, esz);
 }
+static bool on_tensor_cores(const psk_window_shape* sh) { return sh->dtype == PSK_BF16 && sh->path != PSK_PATH_CUDA_CORES; }
 WinArgs args_of(const psk_window_shape* sh) {
     WinArgs a{};
     a.B = sh->B; a.H = sh->H; a.Hkv = sh->Hkv; a.G = sh->H / sh->Hkv; a.n = sh->n;
@@ -454,9 +457,14 @@ int psk_window_attn_fwd(const psk_window_shape* shape, const void* Q, const void
     cudaStream_t s = (cudaStream_t)stream;
     WinArgs a = args_of(shape);
     a.Q = Q; a.K = K; a.V = V; a.out = O; a.lse = lse; a.lengths = lengths;
-    cudaError_t e = cudaMemsetAsync(workspace, 0, sizeof(int), s);
-    if (e == cudaSuccess)
+    int* status = static_cast<int*>(workspace);
+    cudaError_t e;
+    if (on_tensor_cores(shape)) {
+        e = tc_window_fwd(a, status, s);
+    } else {
+        a.status = status;
         e = shape->dtype == PSK_F32 ? cc_window_fwd<float>(a, s) : cc_window_fwd<bf16>(a, s);
+    }
     return e == cudaSuccess ? PSK_OK : PSK_ERR_CUDA;
 }
 
@@ -473,9 +481,14 @@ int psk_window_attn_bwd(const psk_window_shape* shape, const void* Q, const void
     WinArgs a = args_of(shape);
     a.Q = Q; a.K = K; a.V = V; a.O = O; a.lse_in = lse; a.dO = dO; a.dQ = dQ; a.dK = dK; a.dV = dV; a.lengths = lengths;
     a.D = reinterpret_cast<float*>(static_cast<char*>(workspace) + kStatusBytes);
-    cudaError_t e = cudaMemsetAsync(workspace, 0, sizeof(int), s);
-    if (e == cudaSuccess)
+    int* status = static_cast<int*>(workspace);
+    cudaError_t e;
+    if (on_tensor_cores(shape)) {
+        e = tc_window_bwd(a, status, s);
+    } else {
+        a.status = status;
         e = shape->dtype == PSK_F32 ? cc_window_bwd<float>(a, s) : cc_window_bwd<bf16>(a, s);
+    }
     return e == cudaSuccess ? PSK_OK : PSK_ERR_CUDA;
 }
 

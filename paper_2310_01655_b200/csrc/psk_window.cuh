@@ -18,6 +18,7 @@ struct WinArgs {
     const float* lse_in;
     float *lse, *D;                   // D: [B,H,n] scratch, written by the query side, read by the key side
     const int32_t* lengths;           // [B] or null
+    int* status;                      // the call's status word; its first kernel clears it
     int B, H, Hkv, G, n, window, sinks;
     float scale, c;                   // c = scale log2(e)
     int64_t qb, qh, qn, kb, kh, kn;   // element strides of the query-side and of the key-side tensors
@@ -149,6 +150,10 @@ int check_common(const psk_window_shape* sh);         // all but n and the strid
 int check_rows(const psk_window_shape* sh);
 WinArgs args_of(const psk_window_shape* sh);
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// tensor cores (psk_window_tc.cu): bf16
+cudaError_t tc_window_fwd(const WinArgs& a, int* status, cudaStream_t s);
+cudaError_t tc_window_bwd(const WinArgs& a, int* status, cudaStream_t s);
 
 }  // namespace win
 }  // namespace psk

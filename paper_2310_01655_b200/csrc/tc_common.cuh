@@ -11,8 +11,8 @@ namespace psk {
 typedef __nv_bfloat16 bf16;
 
 // host: tensor maps (defined in psk_tc.cu)
-// [B,H,n,64] bf16 rows, box 128 rows x 64 columns, 128-byte swizzle
-bool tc_map_rows(CUtensorMap* m, const void* base, int B, int H, int n, int64_t sb, int64_t sh, int64_t sn);
+// [B,H,n,64] bf16 rows, box box_rows rows x 64 columns, 128-byte swizzle
+bool tc_map_rows(CUtensorMap* m, const void* base, int B, int H, int n, int64_t sb, int64_t sh, int64_t sn, int box_rows = 128);
 // states S[nblk][80][FP] bf16, box 80 rows x 64 features
 bool tc_map_states(CUtensorMap* m, const void* base, int FP, int64_t nblk);
 // row-major [rows][cols] bf16 matrix, box box_rows x 64 columns
