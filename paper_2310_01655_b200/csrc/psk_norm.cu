@@ -7,6 +7,7 @@
 // the forward's bytes).  All sums in fp32, the variance from the deviations (two passes over registers).
 // A row belongs to G = 8, 16 or 32 lanes of a warp, or to a CTA; which, by how many 16-byte accesses it has (a lane keeps up to 32
 // values).  Rows whose address or stride is not a multiple of 16 bytes are read value by value.
+#include "fast_div.cuh"
 #include "psk_internal.cuh"
 
 #include <math.h>
@@ -16,19 +17,6 @@ namespace {
 
 typedef __nv_bfloat16 bf16;
 constexpr int kNormThreads = 256, kNormWarps = kNormThreads / 32, kNormMaxCols = 8192;
-
-// x / d for 0 <= x < 2^31, 0 < d < 2^31 without a division: multiplication by ceil(2^(31 + s) / d), 2^s >= d
-// (the error of the reciprocal times x stays below 1/d).
-struct FastDiv {
-    uint32_t d, mul, shift;
-    void set(uint32_t v) {
-        d = v;
-        shift = 0;
-        while ((1ull << shift) < v) ++shift;
-        mul = v == 1 ? 0 : (uint32_t)(((1ull << (31 + shift)) + v - 1) / v);
-    }
-    __device__ __forceinline__ uint32_t div(uint32_t x) const { return mul == 0 ? x : __umulhi(x, mul) >> (shift - 1); }
-};
 
 struct NormArgs {
     const void *x, *y;                // y: dY (backward only)

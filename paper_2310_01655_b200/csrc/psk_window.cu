@@ -178,12 +178,13 @@ win_fwd_kernel(const __grid_constant__ WinArgs a) {
     }
     __syncthreads();
     for (int r = tid / 32; row0 + r < end && r < kTile; r += kThreads / 32)
-        if (s_bad[r]) redo_out_row(Q + (int64_t)(row0 + r) * a.qn, K, V, a.kn, row0 + r, a.window, a.sinks, a.c, O + (int64_t)(row0 + r) * a.qn, lse + row0 + r);
+        if (s_bad[r]) st2(O + (int64_t)(row0 + r) * a.qn + 2 * (tid % 32),
+                          redo_out_row(Q + (int64_t)(row0 + r) * a.qn, K, V, a.kn, row0 + r, a.window, a.sinks, a.c, lse + row0 + r));
 }
 
 constexpr size_t kDqSmem = 4 * kUnit * sizeof(float);
 
-// The gradient of 64 query rows; their D_i on the way, which the key side reads.
+// The gradient of 64 query rows; their statistics on the way, which the key side reads.
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 win_dq_kernel(const __grid_constant__ WinArgs a) {
@@ -200,7 +201,7 @@ win_dq_kernel(const __grid_constant__ WinArgs a) {
     T* dQ = (T*)a.dQ + qoff;
     const int row0 = pl.row0, len = pl.len, n_end = row0 + kTile < a.n ? row0 + kTile : a.n, end = row0 + kTile < len ? row0 + kTile : len;
     zero_rows(dQ + (int64_t)(end > row0 ? end - row0 : 0) * a.qn, a.qn, row0, n_end - (end > row0 ? end - row0 : 0));
-    for (int r = (end > row0 ? end : row0) + tid; r < n_end; r += kThreads) a.D[soff + r] = 0.f;
+    for (int r = (end > row0 ? end : row0) + tid; r < n_end; r += kThreads) a.stat_l[soff + r] = a.stat_d[soff + r] = 0.f;
     if (end <= row0) return;
     load_tile(sQ, Q, a.qn, row0, end);
     load_tile(sG, dO, a.qn, row0, end);
@@ -212,7 +213,7 @@ win_dq_kernel(const __grid_constant__ WinArgs a) {
         for (int c = 0; c < 64; ++c) D = fmaf(sG[tid * kLd + c], sK[tid * kLd + c], D);
         s_D[tid] = D;
         s_lse[tid] = row0 + tid < end ? a.lse_in[soff + row0 + tid] * kLog2e : 0.f;
-        if (row0 + tid < end) a.D[soff + row0 + tid] = D;
+        if (row0 + tid < end) { a.stat_l[soff + row0 + tid] = -s_lse[tid]; a.stat_d[soff + row0 + tid] = -D; }
     }
     Acc acc;
     acc.zero();
@@ -266,7 +267,7 @@ win_dq_kernel(const __grid_constant__ WinArgs a) {
     for (int r = tid / 32; row0 + r < end && r < kTile; r += kThreads / 32)
         if (s_bad[r]) {
             const int64_t at = (int64_t)(row0 + r) * a.qn;
-            redo_dq_row(Q + at, dO + at, K, V, a.kn, row0 + r, a.window, a.sinks, a.c, a.scale, a.lse_in[soff + row0 + r], s_D[r], dQ + at);
+            st2(dQ + at + 2 * (tid % 32), redo_dq_row(Q + at, dO + at, K, V, a.kn, row0 + r, a.window, a.sinks, a.c, a.scale, make_float2(s_lse[r], s_D[r])));
         }
 }
 
@@ -304,8 +305,8 @@ win_dkv_kernel(const __grid_constant__ WinArgs a) {
             __syncthreads();
             load_tile(sQ, Q, a.qn, i0, len);
             load_tile(sG, dO, a.qn, i0, len);
-            s_D[tid] = i0 + tid < len ? a.D[soff + i0 + tid] : 0.f;
-            s_lse[tid] = i0 + tid < len ? a.lse_in[soff + i0 + tid] * kLog2e : 0.f;
+            s_lse[tid] = i0 + tid < len ? -a.stat_l[soff + i0 + tid] : 0.f;
+            s_D[tid] = i0 + tid < len ? -a.stat_d[soff + i0 + tid] : 0.f;
             __syncthreads();
             // rows: queries; columns: keys
 #pragma unroll
@@ -356,7 +357,11 @@ win_dkv_kernel(const __grid_constant__ WinArgs a) {
     }
     __syncthreads();
     for (int r = tid / 32; key0 + r < end && r < kTile; r += kThreads / 32)
-        if (s_bad[r]) redo_dkv_row<T>(a, pl.b, pl.h, key0 + r, len);
+        if (s_bad[r]) {
+            const KeyRow k = redo_dkv_row<T>(a, pl.b, pl.h, key0 + r, len);
+            st2(dK + (int64_t)(key0 + r) * a.kn + 2 * (tid % 32), k.dk);
+            st2(dV + (int64_t)(key0 + r) * a.kn + 2 * (tid % 32), k.dv);
+        }
 }
 
 template <typename Kern>
@@ -442,7 +447,7 @@ extern "C" {
 
 size_t psk_window_workspace_bytes(const psk_window_shape* shape, int for_backward) {
     if (check_rows(shape) != PSK_OK) return 0;
-    return kStatusBytes + (for_backward ? align_up((size_t)shape->B * shape->H * shape->n * sizeof(float)) : 0);
+    return kStatusBytes + (for_backward ? 2 * align_up((size_t)shape->B * shape->H * shape->n * sizeof(float)) : 0);
 }
 
 int psk_window_attn_fwd(const psk_window_shape* shape, const void* Q, const void* K, const void* V, const int32_t* lengths, void* O, float* lse,
@@ -480,7 +485,8 @@ int psk_window_attn_bwd(const psk_window_shape* shape, const void* Q, const void
     cudaStream_t s = (cudaStream_t)stream;
     WinArgs a = args_of(shape);
     a.Q = Q; a.K = K; a.V = V; a.O = O; a.lse_in = lse; a.dO = dO; a.dQ = dQ; a.dK = dK; a.dV = dV; a.lengths = lengths;
-    a.D = reinterpret_cast<float*>(static_cast<char*>(workspace) + kStatusBytes);
+    a.stat_l = reinterpret_cast<float*>(static_cast<char*>(workspace) + kStatusBytes);
+    a.stat_d = a.stat_l + align_up((size_t)a.B * a.H * a.n * sizeof(float)) / sizeof(float);
     int* status = static_cast<int*>(workspace);
     cudaError_t e;
     if (on_tensor_cores(shape)) {

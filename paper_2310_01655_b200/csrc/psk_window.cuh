@@ -16,7 +16,8 @@ struct WinArgs {
     const void *Q, *K, *V, *O, *dO;
     void *out, *dQ, *dK, *dV;         // `out`: O of the forward
     const float* lse_in;
-    float *lse, *D;                   // D: [B,H,n] scratch, written by the query side, read by the key side
+    float* lse;
+    float *stat_l, *stat_d;           // [B,H,n] scratch: -lse log2(e) and -D, written by the query side, read by the key side
     const int32_t* lengths;           // [B] or null
     int* status;                      // the call's status word; its first kernel clears it
     int B, H, Hkv, G, n, window, sinks;
@@ -64,9 +65,9 @@ __device__ __forceinline__ void for_keys(int i, int window, int sinks, F&& f) {
     for (int j = lo; j <= i; ++j) f(j);
 }
 
-// q, K, V, o: of row i and of its head
+// q, K, V: of row i and of its head; lse: its place, or null
 template <typename T>
-__device__ __noinline__ void redo_out_row(const T* q, const T* K, const T* V, int64_t kn, int i, int window, int sinks, float c, T* o, float* lse) {
+__device__ __noinline__ float2 redo_out_row(const T* q, const T* K, const T* V, int64_t kn, int i, int window, int sinks, float c, float* lse) {
     const int l2 = 2 * (threadIdx.x % 32);
     const float2 qv = ld2(q + l2);
     float m = neg_inf(), l = 0.f;
@@ -81,48 +82,49 @@ __device__ __noinline__ void redo_out_row(const T* q, const T* K, const T* V, in
         l = fmaf(l, alpha, p);
         m = m2;
     });
-    st2(o + l2, make_float2(acc.x / l, acc.y / l));
-    if (l2 == 0) *lse = (m + log2f(l)) * kLn2;
+    if (l2 == 0 && lse != nullptr) *lse = (m + log2f(l)) * kLn2;
+    return make_float2(acc.x / l, acc.y / l);
 }
 
 template <typename T>
-__device__ __noinline__ void redo_dq_row(const T* q, const T* dO, const T* K, const T* V, int64_t kn, int i, int window, int sinks, float c, float scale,
-                                         float lse, float D, T* dq) {
+__device__ __noinline__ float2 redo_dq_row(const T* q, const T* dO, const T* K, const T* V, int64_t kn, int i, int window, int sinks, float c, float scale,
+                                           float2 stat) {
     const int l2 = 2 * (threadIdx.x % 32);
     const float2 qv = ld2(q + l2), dv = ld2(dO + l2);
     float2 acc = make_float2(0.f, 0.f);
     for_keys(i, window, sinks, [&](int j) {
         const float2 k = ld2(K + j * kn + l2);
-        const float p = exp2_approx(dot2(qv, k) * c - lse * kLog2e);
-        const float ds = p * (dot2(dv, ld2(V + j * kn + l2)) - D);
+        const float p = exp2_approx(fmaf(dot2(qv, k), c, -stat.x));
+        const float ds = p * (dot2(dv, ld2(V + j * kn + l2)) - stat.y);
         acc.x = fmaf(ds, k.x, acc.x);
         acc.y = fmaf(ds, k.y, acc.y);
     });
-    st2(dq + l2, make_float2(acc.x * scale, acc.y * scale));
+    return make_float2(acc.x * scale, acc.y * scale);
 }
 
-// row j of key head hk of sequence b
+// row j of key head hk of sequence b: (dk, dv)
+struct KeyRow { float2 dk, dv; };
 template <typename T>
-__device__ __noinline__ void redo_dkv_row(const WinArgs& a, int b, int hk, int j, int len) {
+__device__ __noinline__ KeyRow redo_dkv_row(const WinArgs& a, int b, int hk, int j, int len) {
     const int l2 = 2 * (threadIdx.x % 32);
     const int64_t krow = b * a.kb + hk * a.kh + j * a.kn + l2;
     const float2 k = ld2((const T*)a.K + krow), v = ld2((const T*)a.V + krow);
-    float2 dk = make_float2(0.f, 0.f), dv = dk;
+    KeyRow r{make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
     const int64_t past = (int64_t)j + a.window;
     const int end = (j < a.sinks || past > len) ? len : (int)past;
     for (int g = 0; g < a.G; ++g) {
         const int h = hk * a.G + g;
         for (int i = j; i < end; ++i) {
-            const int64_t row = b * a.qb + h * a.qh + i * a.qn + l2, st = ((int64_t)b * a.H + h) * a.n + i;
+            const int64_t row = b * a.qb + h * a.qh + i * a.qn + l2;
+            const int64_t at = ((int64_t)b * a.H + h) * a.n + i;
             const float2 q = ld2((const T*)a.Q + row), d = ld2((const T*)a.dO + row);
-            const float p = exp2_approx(dot2(q, k) * a.c - a.lse_in[st] * kLog2e);
-            const float ds = p * (dot2(d, v) - a.D[st]) * a.scale;
-            dv.x = fmaf(p, d.x, dv.x); dv.y = fmaf(p, d.y, dv.y);
-            dk.x = fmaf(ds, q.x, dk.x); dk.y = fmaf(ds, q.y, dk.y);
+            const float p = exp2_approx(fmaf(dot2(q, k), a.c, a.stat_l[at]));
+            const float ds = p * (dot2(d, v) + a.stat_d[at]) * a.scale;
+            r.dv.x = fmaf(p, d.x, r.dv.x); r.dv.y = fmaf(p, d.y, r.dv.y);
+            r.dk.x = fmaf(ds, q.x, r.dk.x); r.dk.y = fmaf(ds, q.y, r.dk.y);
         }
     }
-    st2((T*)a.dK + krow, dk);
-    st2((T*)a.dV + krow, dv);
+    return r;
 }
 
 // The key tiles (of `tile` keys) that rows row0 .. row1 see any key of: [0, sink_tiles) and [band0, band1].
