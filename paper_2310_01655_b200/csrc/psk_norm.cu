@@ -5,9 +5,12 @@
 // Bound: memory.  A row is read once and stays in registers; the backward forms mean and rstd again from the x that it
 // reads anyway, so that nothing but x is kept from the forward (for rows of 64 in bf16 two stored floats would be 6 % of
 // the forward's bytes).  All sums in fp32, the variance from the deviations (two passes over registers).
-// A row belongs to G = 8, 16 or 32 lanes of a warp, or to a CTA; which, by how many 16-byte accesses it has (a lane keeps up to 32
-// values).  Rows whose address or stride is not a multiple of 16 bytes are read value by value.
+// A row belongs to G = 4 to 32 lanes of a warp, or to a CTA; which, by how many 16-byte accesses it has (a lane keeps 8 to 32
+// values: a row's own work, its addresses, its sums over lanes, its root, is shared by few lanes).  The next row is on its way while one is
+// worked on.  Values are handled in packed pairs: with scalar arithmetic the issue slots bound the backward of rows of 64 (1.57 M rows: 236 us).
+// Rows whose address or stride is not a multiple of 16 bytes are read value by value.
 #include "fast_div.cuh"
+#include "packed.cuh"
 #include "psk_internal.cuh"
 
 #include <math.h>
@@ -35,28 +38,46 @@ __device__ __forceinline__ int64_t row_offset(const NormArgs& a, const int64_t (
     return (int64_t)i0 * s[0] + (int64_t)i1 * s[1] + (int64_t)i2 * s[2];
 }
 
+// Values are handled in pairs (f2), or one by one where rows are read so.
+template <int V> struct Word { typedef f2 type; };
+template <> struct Word<1> { typedef float type; };
+__device__ __forceinline__ f2 vadd(f2 a, f2 b) { return add2(a, b); }
+__device__ __forceinline__ f2 vmul(f2 a, f2 b) { return mul2(a, b); }
+__device__ __forceinline__ f2 vfma(f2 a, f2 b, f2 c) { return fma2(a, b, c); }
+__device__ __forceinline__ float vsum(f2 a) { return lo2(a) + hi2(a); }
+__device__ __forceinline__ float vat(f2 a, int i) { return i ? hi2(a) : lo2(a); }
+__device__ __forceinline__ void vset(f2& a, float v) { a = pack2(v, v); }
+__device__ __forceinline__ void vload(f2& a, const float* p) { a = pack2(p[0], p[1]); }
+__device__ __forceinline__ float vadd(float a, float b) { return a + b; }
+__device__ __forceinline__ float vmul(float a, float b) { return a * b; }
+__device__ __forceinline__ float vfma(float a, float b, float c) { return fmaf(a, b, c); }
+__device__ __forceinline__ float vsum(float a) { return a; }
+__device__ __forceinline__ float vat(float a, int) { return a; }
+__device__ __forceinline__ void vset(float& a, float v) { a = v; }
+__device__ __forceinline__ void vload(float& a, const float* p) { a = p[0]; }
+
 // V values at p: 16 bytes, or one value
 template <typename T, int V> struct Pack;
 template <> struct Pack<float, 4> {
     float4 v;
     __device__ __forceinline__ void load(const float* p) { v = *reinterpret_cast<const float4*>(p); }
     __device__ __forceinline__ void zero() { v = make_float4(0.f, 0.f, 0.f, 0.f); }
-    __device__ __forceinline__ void get(float* f) const { f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w; }
-    __device__ __forceinline__ static void store(float* p, const float* f) { *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]); }
+    __device__ __forceinline__ void get(f2* f) const { f[0] = pack2(v.x, v.y); f[1] = pack2(v.z, v.w); }
+    __device__ __forceinline__ static void store(float* p, const f2* f) { *reinterpret_cast<float4*>(p) = make_float4(lo2(f[0]), hi2(f[0]), lo2(f[1]), hi2(f[1])); }
 };
 template <> struct Pack<bf16, 8> {
     uint4 v;
     __device__ __forceinline__ void load(const bf16* p) { v = *reinterpret_cast<const uint4*>(p); }
     __device__ __forceinline__ void zero() { v = make_uint4(0, 0, 0, 0); }
-    __device__ __forceinline__ void get(float* f) const {
+    __device__ __forceinline__ void get(f2* f) const {
         const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(u[i] << 16); f[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
+        for (int i = 0; i < 4; ++i) f[i] = pack2(u[i] << 16, u[i] & 0xffff0000u);
     }
-    __device__ __forceinline__ static void store(bf16* p, const float* f) {
+    __device__ __forceinline__ static void store(bf16* p, const f2* f) {
         uint32_t u[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(u[i]) : "f"(f[2 * i + 1]), "f"(f[2 * i]));
+        for (int i = 0; i < 4; ++i) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(u[i]) : "f"(hi2(f[i])), "f"(lo2(f[i])));
         *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
     }
 };
@@ -68,25 +89,25 @@ template <typename T> struct Pack<T, 1> {
     __device__ __forceinline__ static void store(T* p, const float* f) { stf(p, f[0]); }
 };
 
-// Sums of N values over the lanes of a row, in every lane.  `red`: shared memory for the rows of a whole CTA; callers alternate
-// between two of them, so that one barrier per sum is enough.
+// Sums of N values over the lanes of a row, in every lane.  `red`: shared memory for the rows of several warps, which meet at a
+// barrier of their own; callers alternate between two of them, so that one barrier per sum is enough.
 template <int G, int N>
 __device__ __forceinline__ void row_sums(float (&s)[N], float (*red)[kNormWarps]) {
-    constexpr int W = G < 32 ? G : 32;
 #pragma unroll
-    for (int o = W / 2; o > 0; o >>= 1)
+    for (int o = (G < 32 ? G : 32) / 2; o > 0; o >>= 1)
 #pragma unroll
         for (int i = 0; i < N; ++i) s[i] += __shfl_xor_sync(0xffffffffu, s[i], o);
     if constexpr (G > 32) {
+        const int group = threadIdx.x / G;
         if (threadIdx.x % 32 == 0)
 #pragma unroll
             for (int i = 0; i < N; ++i) red[i][threadIdx.x / 32] = s[i];
-        __syncthreads();
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(G) : "memory");
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             s[i] = 0.f;
 #pragma unroll
-            for (int w = 0; w < kNormWarps; ++w) s[i] += red[i][w];
+            for (int w = 0; w < G / 32; ++w) s[i] += red[i][group * (G / 32) + w];
         }
     }
 }
@@ -97,186 +118,235 @@ __device__ __forceinline__ float over_cols(const NormArgs& a, float s) {
     return fmaf(fmaf(-m, (float)a.cols, s), a.over_cols, m);
 }
 
-// A row's lanes, and what they hold: accesses l, l + G, ... of V values each.
+// A row's lanes, and what they hold: accesses l, l + G, ... of V values each, as kPer words each.
 template <int V, int NV, int G> struct RowMap {
-    static constexpr int kRowsPerCta = kNormThreads / G, kValues = V * NV;
-    static constexpr int kUnroll = NV == 1 ? (G < 32 ? 4 : 2) : 1;        // rows in flight per lane
+    static constexpr int kRowsPerCta = kNormThreads / G, kPer = (V + 1) / 2, kPairs = kPer * NV, kValues = V * NV;
+    // rows in flight per lane, as registers allow
+    static constexpr int kFwdRows = kValues <= 8 ? 4 : (kValues <= 16 ? 4 : 3), kBwdRows = kValues <= 16 ? 2 : 1;
 };
-
+// a parameter's values at the lane's columns (1 or 0 where there is none)
+template <int V> __device__ __forceinline__ void load_param(typename Word<V>::type* f, const float* p, int vec, bool in, float none) {
+#pragma unroll
+    for (int i = 0; i < (V + 1) / 2; ++i) {
+        if (in && p != nullptr) vload(f[i], p + vec * V + 2 * i);
+        else vset(f[i], none);
+    }
+}
 template <typename T, int V, int NV, int G>
-__global__ void __launch_bounds__(kNormThreads)
-norm_fwd_kernel(const __grid_constant__ NormArgs a) {
-    using M = RowMap<V, NV, G>;
-    constexpr int U = M::kUnroll;
-    __shared__ float red[2][1][kNormWarps];
-    pdl_sync();
-    const int l = threadIdx.x % G, group = threadIdx.x / G, nvec = a.cols / V;
-    float gain[M::kValues], bias[M::kValues];
+__device__ __forceinline__ void load_row(Pack<T, V> (&x)[NV], const NormArgs& a, const void* base, const int64_t (&strides)[3], uint64_t r, int l, int nvec) {
+    const T* row = (const T*)base + (r < a.rows ? row_offset(a, strides, (uint32_t)r) : 0);
 #pragma unroll
-    for (int k = 0; k < NV; ++k)
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int vec = l + k * G, c = vec * V + i;
-            gain[k * V + i] = (vec < nvec && a.gain != nullptr) ? a.gain[c] : 1.f;
-            bias[k * V + i] = (vec < nvec && a.bias != nullptr) ? a.bias[c] : 0.f;
-        }
-    const uint64_t step = (uint64_t)gridDim.x * M::kRowsPerCta;
-    // (the loop's bound is the same for all lanes of a CTA: rows beyond the last are computed as zeros and not stored)
-    for (uint64_t r0 = (uint64_t)blockIdx.x * M::kRowsPerCta; r0 < a.rows; r0 += step * U) {
-        Pack<T, V> x[U][NV];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const uint64_t r = r0 + u * step + group;
-            const T* row = (const T*)a.x + (r < a.rows ? row_offset(a, a.xs, (uint32_t)r) : 0);
-#pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                const int vec = l + k * G;
-                if (r < a.rows && vec < nvec) x[u][k].load(row + vec * V); else x[u][k].zero();
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const uint64_t r = r0 + u * step + group;
-            float f[M::kValues], s[1] = {0.f}, q[1] = {0.f};
-#pragma unroll
-            for (int k = 0; k < NV; ++k) x[u][k].get(f + k * V);
-#pragma unroll
-            for (int i = 0; i < M::kValues; ++i) s[0] += f[i];
-            row_sums<G>(s, red[0]);
-            const float mean = over_cols(a, s[0]);
-#pragma unroll
-            for (int k = 0; k < NV; ++k)
-                if (l + k * G < nvec)
-#pragma unroll
-                    for (int i = 0; i < V; ++i) { f[k * V + i] -= mean; q[0] = fmaf(f[k * V + i], f[k * V + i], q[0]); }
-            row_sums<G>(q, red[1]);
-            const float rstd = 1.f / sqrtf(q[0] * a.over_cols + a.eps);
-            if (r < a.rows) {
-                T* row = (T*)a.z + row_offset(a, a.zs, (uint32_t)r);
-#pragma unroll
-                for (int k = 0; k < NV; ++k) {
-                    const int vec = l + k * G;
-#pragma unroll
-                    for (int i = 0; i < V; ++i) f[k * V + i] = fmaf(f[k * V + i] * rstd, gain[k * V + i], bias[k * V + i]);
-                    if (vec < nvec) Pack<T, V>::store(row + vec * V, f + k * V);
-                }
-            }
-        }
+    for (int k = 0; k < NV; ++k) {
+        const int vec = l + k * G;
+        if (r < a.rows && vec < nvec) x[k].load(row + vec * V); else x[k].zero();
     }
 }
 
 template <typename T, int V, int NV, int G>
 __global__ void __launch_bounds__(kNormThreads)
+norm_fwd_kernel(const __grid_constant__ NormArgs a) {
+    using M = RowMap<V, NV, G>;
+    typedef typename Word<V>::type W;
+    constexpr int P = M::kPer, D = M::kFwdRows;
+    constexpr bool kKeep = M::kValues <= 24;              // gain and bias in registers, or read again for every row (from L1)
+    __shared__ float red[2][1][kNormWarps];
+    pdl_sync();
+    const int l = threadIdx.x % G, group = threadIdx.x / G, nvec = a.cols / V;
+    W gain[kKeep ? M::kPairs : 1], bias[kKeep ? M::kPairs : 1];
+    if constexpr (kKeep)
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int vec = l + k * G;
+            load_param<V>(gain + k * P, a.gain, vec, vec < nvec, 1.f);
+            load_param<V>(bias + k * P, a.bias, vec, vec < nvec, 0.f);
+        }
+    const uint64_t step = (uint64_t)gridDim.x * M::kRowsPerCta;
+    Pack<T, V> next[D][NV];
+    uint64_t r = (uint64_t)blockIdx.x * M::kRowsPerCta + group;
+#pragma unroll
+    for (int d = 0; d < D; ++d) load_row<T, V, NV, G>(next[d], a, a.x, a.xs, r + d * step, l, nvec);
+    // (the number of rounds is the same for all lanes of a CTA: rows beyond the last are computed as zeros and not stored)
+    for (uint64_t r0 = (uint64_t)blockIdx.x * M::kRowsPerCta; r0 < a.rows; r0 += D * step) {
+#pragma unroll
+      for (int d = 0; d < D; ++d, r += step) {
+        if (r0 + d * step >= a.rows) break;
+        W f[M::kPairs];
+#pragma unroll
+        for (int k = 0; k < NV; ++k) next[d][k].get(f + k * P);
+        load_row<T, V, NV, G>(next[d], a, a.x, a.xs, r + D * step, l, nvec);
+        W s2, q2;
+        vset(s2, 0.f);
+        vset(q2, 0.f);
+#pragma unroll
+        for (int i = 0; i < M::kPairs; ++i) s2 = vadd(s2, f[i]);
+        float s[1] = {vsum(s2)};
+        row_sums<G>(s, red[0]);
+        const float mean = over_cols(a, s[0]);
+        W mean2;
+        vset(mean2, -mean);
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            if (l + k * G < nvec)
+#pragma unroll
+                for (int i = 0; i < P; ++i) { W& v = f[k * P + i]; v = vadd(v, mean2); q2 = vfma(v, v, q2); }
+        float q[1] = {vsum(q2)};
+        row_sums<G>(q, red[1]);
+        const float rstd = rsqrtf(fmaf(q[0], a.over_cols, a.eps));
+        W rstd2;
+        vset(rstd2, rstd);
+        if (r < a.rows) {
+            T* row = (T*)a.z + row_offset(a, a.zs, (uint32_t)r);
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                const int vec = l + k * G;
+                if (vec >= nvec) continue;
+                W g[P], b[P];
+                if constexpr (kKeep) {
+#pragma unroll
+                    for (int i = 0; i < P; ++i) { g[i] = gain[k * P + i]; b[i] = bias[k * P + i]; }
+                } else {
+                    load_param<V>(g, a.gain, vec, true, 1.f);
+                    load_param<V>(b, a.bias, vec, true, 0.f);
+                }
+#pragma unroll
+                for (int i = 0; i < P; ++i) f[k * P + i] = vfma(vmul(f[k * P + i], rstd2), g[i], b[i]);
+                Pack<T, V>::store(row + vec * V, f + k * P);
+            }
+        }
+      }
+    }
+}
+
+template <typename T, int V, int NV, int G>
+__global__ void __launch_bounds__(kNormThreads, RowMap<V, NV, G>::kValues <= 16 ? 2 : 1)
 norm_bwd_kernel(const __grid_constant__ NormArgs a) {
     using M = RowMap<V, NV, G>;
-    constexpr int U = M::kUnroll > 2 ? 2 : M::kUnroll;
+    typedef typename Word<V>::type W;
+    constexpr int P = M::kPer, D = M::kBwdRows;
+    constexpr bool kKeep = M::kValues <= 16;
     __shared__ float red1[1][kNormWarps], red2[3][kNormWarps];
     extern __shared__ float sums[];                                       // [2][cols]
     pdl_sync();
     const int l = threadIdx.x % G, group = threadIdx.x / G, nvec = a.cols / V;
-    float dg[M::kValues], db[M::kValues];
+    W dg[M::kPairs], db[M::kPairs], gain[kKeep ? M::kPairs : 1];
 #pragma unroll
-    for (int i = 0; i < M::kValues; ++i) dg[i] = db[i] = 0.f;
-    // the gain stays in registers where a lane has few values; otherwise it is read again for every row (from L1)
-    constexpr bool kKeep = M::kValues <= 16;
-    float gain[kKeep ? M::kValues : 1];
+    for (int i = 0; i < M::kPairs; ++i) { vset(dg[i], 0.f); vset(db[i], 0.f); }
     if constexpr (kKeep)
 #pragma unroll
-        for (int i = 0; i < M::kValues; ++i) {
-            const int vec = l + i / V * G;
-            gain[i] = (vec < nvec && a.gain != nullptr) ? a.gain[vec * V + i % V] : 1.f;
-        }
+        for (int k = 0; k < NV; ++k) load_param<V>(gain + k * P, a.gain, l + k * G, l + k * G < nvec, 1.f);
     const uint64_t step = (uint64_t)gridDim.x * M::kRowsPerCta;
-    for (uint64_t r0 = (uint64_t)blockIdx.x * M::kRowsPerCta; r0 < a.rows; r0 += step * U) {
-        Pack<T, V> x[U][NV], y[U][NV];
+    Pack<T, V> nx[D][NV], ny[D][NV];
+    uint64_t r = (uint64_t)blockIdx.x * M::kRowsPerCta + group;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const uint64_t r = r0 + u * step + group;
-            const T* xrow = (const T*)a.x + (r < a.rows ? row_offset(a, a.xs, (uint32_t)r) : 0);
-            const T* yrow = (const T*)a.y + (r < a.rows ? row_offset(a, a.ys, (uint32_t)r) : 0);
+    for (int d = 0; d < D; ++d) {
+        load_row<T, V, NV, G>(nx[d], a, a.x, a.xs, r + d * step, l, nvec);
+        load_row<T, V, NV, G>(ny[d], a, a.y, a.ys, r + d * step, l, nvec);
+    }
+    for (uint64_t r0 = (uint64_t)blockIdx.x * M::kRowsPerCta; r0 < a.rows; r0 += D * step) {
 #pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                const int vec = l + k * G;
-                if (r < a.rows && vec < nvec) { x[u][k].load(xrow + vec * V); y[u][k].load(yrow + vec * V); }
-                else { x[u][k].zero(); y[u][k].zero(); }
+      for (int d = 0; d < D; ++d, r += step) {
+        if (r0 + d * step >= a.rows) break;
+        Pack<T, V> x[NV], y[NV];
+#pragma unroll
+        for (int k = 0; k < NV; ++k) { x[k] = nx[d][k]; y[k] = ny[d][k]; }
+        load_row<T, V, NV, G>(nx[d], a, a.x, a.xs, r + D * step, l, nvec);
+        load_row<T, V, NV, G>(ny[d], a, a.y, a.ys, r + D * step, l, nvec);
+        W s2;
+        vset(s2, 0.f);
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            W f[P];
+            x[k].get(f);
+#pragma unroll
+            for (int i = 0; i < P; ++i) s2 = vadd(s2, f[i]);
+        }
+        float s[1] = {vsum(s2)};
+        row_sums<G>(s, red1);
+        const float mean = over_cols(a, s[0]);
+        W mean2;
+        vset(mean2, -mean);
+        // sums of the squared deviations, of g = dy gain, and of g times the deviation
+        W t2[3];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) vset(t2[i], 0.f);
+        auto gained = [&](W (&g)[P], const W (&d)[P], int k) {
+            if constexpr (kKeep) {
+#pragma unroll
+                for (int i = 0; i < P; ++i) g[i] = vmul(d[i], gain[k * P + i]);
+            } else {
+                load_param<V>(g, a.gain, l + k * G, true, 1.f);
+#pragma unroll
+                for (int i = 0; i < P; ++i) g[i] = vmul(d[i], g[i]);
+            }
+        };
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            if (l + k * G >= nvec) continue;
+            W f[P], d[P], g[P];
+            x[k].get(f);
+            y[k].get(d);
+            gained(g, d, k);
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                const W dev = vadd(f[i], mean2);
+                t2[0] = vfma(dev, dev, t2[0]);
+                t2[1] = vadd(t2[1], g[i]);
+                t2[2] = vfma(g[i], dev, t2[2]);
             }
         }
+        float t[3];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const uint64_t r = r0 + u * step + group;
-            float s[1] = {0.f};
-#pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                float f[V];
-                x[u][k].get(f);
-#pragma unroll
-                for (int i = 0; i < V; ++i) s[0] += f[i];
-            }
-            row_sums<G>(s, red1);
-            const float mean = over_cols(a, s[0]);
-            // sums of the squared deviations, of a = dy gain, and of a times the deviation
-            float t[3] = {0.f, 0.f, 0.f};
+        for (int i = 0; i < 3; ++i) t[i] = vsum(t2[i]);
+        row_sums<G>(t, red2);
+        const float rstd = rsqrtf(fmaf(t[0], a.over_cols, a.eps));
+        // dx = rstd g - rstd sum(g) / C - dev rstd^3 sum(g dev) / C
+        const float k1 = -rstd * t[1] * a.over_cols, k2 = -rstd * rstd * rstd * (t[2] * a.over_cols);
+        W rstd2, k12, k22;
+        vset(rstd2, rstd);
+        vset(k12, k1);
+        vset(k22, k2);
+        if (r < a.rows) {
+            T* row = (T*)a.z + row_offset(a, a.zs, (uint32_t)r);
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
                 const int vec = l + k * G;
-                float f[V], d[V];
-                x[u][k].get(f);
-                y[u][k].get(d);
-                if (vec < nvec)
+                if (vec >= nvec) continue;
+                W f[P], d[P], g[P];
+                x[k].get(f);
+                y[k].get(d);
+                gained(g, d, k);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        const float dev = f[i] - mean;
-                        const float ag = d[i] * (kKeep ? gain[kKeep ? k * V + i : 0] : (a.gain != nullptr ? a.gain[vec * V + i] : 1.f));
-                        t[0] = fmaf(dev, dev, t[0]);
-                        t[1] += ag;
-                        t[2] = fmaf(ag, dev, t[2]);
-                    }
-            }
-            row_sums<G>(t, red2);
-            const float rstd = 1.f / sqrtf(t[0] * a.over_cols + a.eps);
-            const float m1 = t[1] * a.over_cols, m2 = t[2] * a.over_cols * rstd;
-            if (r < a.rows) {
-                T* row = (T*)a.z + row_offset(a, a.zs, (uint32_t)r);
-#pragma unroll
-                for (int k = 0; k < NV; ++k) {
-                    const int vec = l + k * G;
-                    float f[V], d[V];
-                    x[u][k].get(f);
-                    y[u][k].get(d);
-                    if (vec < nvec) {
-#pragma unroll
-                        for (int i = 0; i < V; ++i) {
-                            const float xhat = (f[i] - mean) * rstd;
-                            const float ag = d[i] * (kKeep ? gain[kKeep ? k * V + i : 0] : (a.gain != nullptr ? a.gain[vec * V + i] : 1.f));
-                            dg[k * V + i] = fmaf(d[i], xhat, dg[k * V + i]);
-                            db[k * V + i] += d[i];
-                            f[i] = rstd * (ag - m1 - xhat * m2);
-                        }
-                        Pack<T, V>::store(row + vec * V, f);
-                    }
+                for (int i = 0; i < P; ++i) {
+                    const W dev = vadd(f[i], mean2);
+                    dg[k * P + i] = vfma(vmul(d[i], rstd2), dev, dg[k * P + i]);
+                    db[k * P + i] = vadd(db[k * P + i], d[i]);
+                    f[i] = vfma(dev, k22, vfma(g[i], rstd2, k12));
                 }
+                Pack<T, V>::store(row + vec * V, f);
             }
         }
+      }
     }
     if (a.dgain == nullptr && a.dbias == nullptr) return;
     // this CTA's sums over its rows: the rows side by side in a warp first, then warp after warp (a fixed order)
 #pragma unroll
     for (int o = G; o < 32; o <<= 1)
 #pragma unroll
-        for (int i = 0; i < M::kValues; ++i) {
-            dg[i] += __shfl_xor_sync(0xffffffffu, dg[i], o);
-            db[i] += __shfl_xor_sync(0xffffffffu, db[i], o);
+        for (int i = 0; i < M::kPairs; ++i) {
+            dg[i] = vadd(dg[i], __shfl_xor_sync(0xffffffffu, dg[i], o));
+            db[i] = vadd(db[i], __shfl_xor_sync(0xffffffffu, db[i], o));
         }
-    constexpr int kTurns = G > 32 ? 1 : kNormWarps;
+    constexpr int kTurns = G > 32 ? kNormThreads / G : kNormWarps;
+    const int turn = G > 32 ? group : (int)threadIdx.x / 32;
     const bool first_rows = G > 32 || threadIdx.x % 32 < G;
     for (int w = 0; w < kTurns; ++w) {
-        if (first_rows && (G > 32 || (int)threadIdx.x / 32 == w))
+        if (first_rows && turn == w)
 #pragma unroll
             for (int i = 0; i < M::kValues; ++i) {
-                const int vec = l + i / V * G, c = vec * V + i % V;
+                const int vec = l + i / V * G, c = vec * V + i % V, at = i / V * P + i % V / 2;
                 if (vec < nvec) {
-                    sums[c] = (w > 0 ? sums[c] : 0.f) + dg[i];
-                    sums[a.cols + c] = (w > 0 ? sums[a.cols + c] : 0.f) + db[i];
+                    sums[c] = (w > 0 ? sums[c] : 0.f) + vat(dg[at], i % V % 2);
+                    sums[a.cols + c] = (w > 0 ? sums[a.cols + c] : 0.f) + vat(db[at], i % V % 2);
                 }
             }
         __syncthreads();
@@ -319,7 +389,7 @@ norm_sum_kernel(const float* __restrict__ partial, int parts, int cols, float* _
 
 // ---- host ----
 
-constexpr int kNormMaxCtas = 148 * 4;
+constexpr int kNormMaxCtas = 148 * 2;           // (with rows in flight two per SM are enough, and fewer sums are left to add up)
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -365,17 +435,11 @@ int check_shape(const psk_norm_shape* sh, bool backward) {
     return rows_apart(n, backward ? sh->zs : sh->ys, sh->cols) ? PSK_OK : PSK_ERR_SHAPE;
 }
 
-int grid_for(uint64_t rows, int rows_per_cta, int unroll) {
-    const uint64_t per = (uint64_t)rows_per_cta * unroll, want = (rows + per - 1) / per;
-    return (int)(want < (uint64_t)kNormMaxCtas ? want : (uint64_t)kNormMaxCtas);
-}
-
 template <typename T, int V, int NV, int G>
 cudaError_t launch(const NormArgs& a, bool backward, cudaStream_t s) {
     using M = RowMap<V, NV, G>;
-    // (rows in flight only once every SM has its CTAs)
-    const uint64_t full = (uint64_t)kNormMaxCtas * M::kRowsPerCta;
-    const int grid = grid_for(a.rows, M::kRowsPerCta, a.rows > full ? 2 : 1);
+    const uint64_t want = ((uint64_t)a.rows + M::kRowsPerCta - 1) / M::kRowsPerCta;
+    const int grid = (int)(want < (uint64_t)kNormMaxCtas ? want : (uint64_t)kNormMaxCtas);
     if (!backward) {
         prof_begin("norm_fwd_kernel", s);
         launch_pdl(norm_fwd_kernel<T, V, NV, G>, dim3(grid), dim3(kNormThreads), 0, s, a);
@@ -404,27 +468,25 @@ cudaError_t dispatch(const NormArgs& a, bool vec, bool backward, cudaStream_t s)
     if (!vec) {
         if (nvec <= 32) return launch<T, 1, 1, 32>(a, backward, s);
         if (nvec <= 128) return launch<T, 1, 4, 32>(a, backward, s);
-        if (nvec <= 512) return launch<T, 1, 16, 32>(a, backward, s);
-        if (nvec <= 1024) return launch<T, 1, 32, 32>(a, backward, s);
-        if (nvec <= 4096) return launch<T, 1, 16, kNormThreads>(a, backward, s);
-        return launch<T, 1, 32, kNormThreads>(a, backward, s);
+        if (nvec <= 256) return launch<T, 1, 8, 32>(a, backward, s);
+        if (nvec <= 512) return launch<T, 1, 8, 64>(a, backward, s);
+        if (nvec <= 1024) return launch<T, 1, 8, 128>(a, backward, s);
+        if (nvec <= 2048) return launch<T, 1, 8, 256>(a, backward, s);
+        if (nvec <= 4096) return launch<T, 1, 16, 256>(a, backward, s);
+        return launch<T, 1, 32, 256>(a, backward, s);
     }
-    if (nvec <= 8) return launch<T, V, 1, 8>(a, backward, s);
-    if (nvec <= 16) return launch<T, V, 1, 16>(a, backward, s);
-    if (nvec <= 32) return launch<T, V, 1, 32>(a, backward, s);
+    if (nvec <= 8) return launch<T, V, 2, 4>(a, backward, s);
+    if (nvec <= 16) return launch<T, V, 2, 8>(a, backward, s);
+    if (nvec <= 32) return launch<T, V, 2, 16>(a, backward, s);
     if (nvec <= 64) return launch<T, V, 2, 32>(a, backward, s);
-    if (nvec <= 96) return launch<T, V, 3, 32>(a, backward, s);
-    if (nvec <= 128) return launch<T, V, 4, 32>(a, backward, s);
-    if constexpr (V == 4) {
-        if (nvec <= 192) return launch<T, V, 6, 32>(a, backward, s);
-        if (nvec <= 256) return launch<T, V, 8, 32>(a, backward, s);
-        if (nvec <= 1024) return launch<T, V, 4, kNormThreads>(a, backward, s);
-        return launch<T, V, 8, kNormThreads>(a, backward, s);
-    } else {
-        if (nvec <= 256) return launch<T, V, 1, kNormThreads>(a, backward, s);
-        if (nvec <= 512) return launch<T, V, 2, kNormThreads>(a, backward, s);
-        return launch<T, V, 4, kNormThreads>(a, backward, s);
-    }
+    // (the forward has the registers for more values in a lane; 65 536 rows of 768, us with 32 / 64 lanes to a row: forward 44 / 57, backward 179 / 85)
+    if (!backward && nvec <= 96) return launch<T, V, 3, 32>(a, backward, s);
+    if (nvec <= 128) return launch<T, V, 2, 64>(a, backward, s);
+    if (nvec <= 256) return launch<T, V, 2, 128>(a, backward, s);
+    if (nvec <= 512) return launch<T, V, 2, 256>(a, backward, s);
+    if (nvec <= 1024) return launch<T, V, 4, 256>(a, backward, s);
+    if constexpr (V == 4) return launch<T, V, 8, 256>(a, backward, s);
+    return cudaErrorInvalidValue;
 }
 
 int run(const psk_norm_shape* sh, NormArgs& a, bool backward, cudaStream_t s) {
