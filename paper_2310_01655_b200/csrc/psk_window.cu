@@ -19,23 +19,30 @@ using namespace cc;
 // ---------------------------------------------------------------------------
 constexpr int kTile = 64, kThreads = 64;
 
-// 64 rows x 64 columns from row r0 into [64][kLd] fp32, zeros from row `end` on
-template <typename T>
+// ROWS rows x 64 columns from row r0 into [ROWS][kLd] fp32, zeros from row `end` on.  fp32: asynchronous copies, all on their way at once (forward
+// of 24 heads x 2048 rows, window 256: 190 us; through registers, in batches of four, 215); cp_wait<> before the barrier in front of their use.
+template <int ROWS = kTile, typename T>
 __device__ __forceinline__ void load_tile(float* dst, const T* src, int64_t stride, int r0, int end) {
     constexpr int V = 16 / sizeof(T), PerRow = 64 / V;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll 8
+        for (int e = threadIdx.x; e < ROWS * PerRow; e += kThreads) {
+            const int r = e / PerRow, c = e % PerRow * V, bytes = r0 + r < end ? 16 : 0;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((unsigned)__cvta_generic_to_shared(dst + r * kLd + c)),
+                         "l"(src + (bytes ? (int64_t)(r0 + r) * stride + c : 0)), "r"(bytes) : "memory");
+        }
+        cp_commit();
+        return;
+    }
 #pragma unroll 4
-    for (int e = threadIdx.x; e < kTile * PerRow; e += kThreads) {
+    for (int e = threadIdx.x; e < ROWS * PerRow; e += kThreads) {
         const int r = e / PerRow, c = e % PerRow * V;
         float* d = dst + r * kLd + c;
         uint4 u = make_uint4(0, 0, 0, 0);
         if (r0 + r < end) u = *reinterpret_cast<const uint4*>(src + (int64_t)(r0 + r) * stride + c);
-        if constexpr (sizeof(T) == 4) {
-            *reinterpret_cast<uint4*>(d) = u;
-        } else {
-            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) *reinterpret_cast<float2*>(d + 2 * i) = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
-        }
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<float2*>(d + 2 * i) = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
     }
 }
 template <typename T>
@@ -68,6 +75,11 @@ __device__ __forceinline__ void zero_rows(T* p, int64_t stride, int r0, int end)
         if (r0 + e / 16 < end) store4(p + (int64_t)(r0 + e / 16) * stride + e % 16 * 4, 0.f, 0.f, 0.f, 0.f);
 }
 
+// Do the `rows` rows from i_first on see all of the keys k0 .. k0 + tile - 1?
+__device__ __forceinline__ bool sees_all(int i_first, int rows, int k0, int tile, int window, int sinks) {
+    return k0 + tile - 1 <= i_first && (window_start(i_first + rows - 1, window) <= k0 || sinks - k0 >= tile);
+}
+
 struct Place { int b, h, row0, len; };
 __device__ __forceinline__ Place place_of(const WinArgs& a, int heads) {
     const int tiles = (a.n + kTile - 1) / kTile, bh = blockIdx.x / tiles;
@@ -79,7 +91,7 @@ __device__ __forceinline__ Place place_of(const WinArgs& a, int heads) {
     return p;
 }
 
-constexpr size_t kFwdSmem = 3 * kUnit * sizeof(float);
+constexpr size_t kFwdSmem = 4 * kUnit * sizeof(float);
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
@@ -89,7 +101,7 @@ win_fwd_kernel(const __grid_constant__ WinArgs a) {
     extern __shared__ float sm[];
     __shared__ float s_al[kTile], s_inv[kTile];
     __shared__ int s_bad[kTile];
-    float *sQ = sm, *sK = sm + kUnit, *sV = sm + 2 * kUnit, *sP = sK;         // the weights take the keys' place
+    float *sQ = sm, *sK = sm + kUnit, *sV = sm + 2 * kUnit, *sP = sm + 3 * kUnit;
     const int tid = threadIdx.x, ry = tid / 8, cx = tid % 8;
     const Place pl = place_of(a, a.H);
     const T* Q = (const T*)a.Q + pl.b * a.qb + pl.h * a.qh;
@@ -109,12 +121,14 @@ win_fwd_kernel(const __grid_constant__ WinArgs a) {
     Acc acc;
     acc.zero();
     const KeyTiles kt = key_tiles(row0, end - 1, a.window, a.sinks, kTile);
-    for (int x = 0; x < kt.count(); ++x) {
+    const int steps = kt.count();
+    load_tile(sK, K, a.kn, kt.at(0) * kTile, len);
+    load_tile(sV, V, a.kn, kt.at(0) * kTile, len);
+    for (int x = 0; x < steps; ++x) {
         const int k0 = kt.at(x) * kTile;
+        cp_wait<1>();                                     // the keys; the values may still be on their way
         __syncthreads();
-        load_tile(sK, K, a.kn, k0, len);
-        load_tile(sV, V, a.kn, k0, len);
-        __syncthreads();
+        const bool whole = sees_all(row0, kTile, k0, kTile, a.window, a.sinks);
         float p[8][8];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
@@ -127,7 +141,7 @@ win_fwd_kernel(const __grid_constant__ WinArgs a) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const float s = sum2(d[i4][j]) * a.c;
-                    p[i][j] = sees(row, k0 + cx + 8 * j, a.window, a.sinks) ? s : neg_inf();
+                    p[i][j] = whole || sees(row, k0 + cx + 8 * j, a.window, a.sinks) ? s : neg_inf();
                     top = fmaxf(top, p[i][j]);
                 }
 #pragma unroll
@@ -140,12 +154,13 @@ win_fwd_kernel(const __grid_constant__ WinArgs a) {
                 if (cx == 0) s_al[ry + 8 * i] = alpha;
             }
         }
-        __syncthreads();                                  // everyone has read the keys
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) sP[(cx + 8 * j) * kLd + ry + 8 * i] = p[i][j];
-        __syncthreads();
+        cp_wait<0>();                                     // the values
+        __syncthreads();                                  // everyone has read the keys
+        if (x + 1 < steps) load_tile(sK, K, a.kn, kt.at(x + 1) * kTile, len);
 #pragma unroll
         for (int p2 = 0; p2 < 4; ++p2) {
             const f2 al = *reinterpret_cast<const f2*>(s_al + 8 * ry + 2 * p2);
@@ -153,6 +168,8 @@ win_fwd_kernel(const __grid_constant__ WinArgs a) {
             for (int q = 0; q < 4; ++q) { acc.s[p2][q] = mul2(acc.s[p2][q], al); acc.x[p2][q] = mul2(acc.x[p2][q], al); }
         }
         outer_product(acc, sP, sV, kTile, kLd, ry, cx);
+        __syncthreads();
+        if (x + 1 < steps) load_tile(sV, V, a.kn, kt.at(x + 1) * kTile, len);
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -182,7 +199,10 @@ win_fwd_kernel(const __grid_constant__ WinArgs a) {
                           redo_out_row(Q + (int64_t)(row0 + r) * a.qn, K, V, a.kn, row0 + r, a.window, a.sinks, a.c, lse + row0 + r));
 }
 
-constexpr size_t kDqSmem = 4 * kUnit * sizeof(float);
+// Keys (query side) or query rows (key side) of a step of the backward: with 32 four CTAs (three) fit into an SM, with 64 three (two):
+// 24 heads x 2048 rows, window 256: 247 + 412 us against 278 + 442.
+constexpr int kStep = 32;
+constexpr size_t kDqSmem = 3 * kUnit * sizeof(float);
 
 // The gradient of 64 query rows; their statistics on the way, which the key side reads.
 template <typename T>
@@ -193,7 +213,7 @@ win_dq_kernel(const __grid_constant__ WinArgs a) {
     extern __shared__ float sm[];
     __shared__ float s_D[kTile], s_lse[kTile];
     __shared__ int s_bad[kTile];
-    float *sQ = sm, *sG = sm + kUnit, *sK = sm + 2 * kUnit, *sV = sm + 3 * kUnit, *sP = sV;      // ds takes the values' place
+    float *sQ = sm, *sG = sm + kUnit, *sK = sm + 2 * kUnit, *sV = sK + kStep * kLd, *sP = sV;      // ds takes the values' place
     const int tid = threadIdx.x, ry = tid / 8, cx = tid % 8;
     const Place pl = place_of(a, a.H);
     const int64_t qoff = pl.b * a.qb + pl.h * a.qh, koff = pl.b * a.kb + pl.h / a.G * a.kh, soff = ((int64_t)pl.b * a.H + pl.h) * a.n;
@@ -206,6 +226,7 @@ win_dq_kernel(const __grid_constant__ WinArgs a) {
     load_tile(sQ, Q, a.qn, row0, end);
     load_tile(sG, dO, a.qn, row0, end);
     load_tile(sK, O, a.qn, row0, end);
+    cp_wait<0>();
     __syncthreads();
     {
         float D = 0.f;
@@ -217,41 +238,41 @@ win_dq_kernel(const __grid_constant__ WinArgs a) {
     }
     Acc acc;
     acc.zero();
-    const KeyTiles kt = key_tiles(row0, end - 1, a.window, a.sinks, kTile);
+    const KeyTiles kt = key_tiles(row0, end - 1, a.window, a.sinks, kStep);
     for (int x = 0; x < kt.count(); ++x) {
-        const int k0 = kt.at(x) * kTile;
+        const int k0 = kt.at(x) * kStep;
         __syncthreads();
-        load_tile(sK, K, a.kn, k0, len);
-        load_tile(sV, V, a.kn, k0, len);
+        load_tile<kStep>(sK, K, a.kn, k0, len);
+        load_tile<kStep>(sV, V, a.kn, k0, len);
+        cp_wait<0>();
         __syncthreads();
-        float ds[8][8];
+        const bool whole = sees_all(row0, kTile, k0, kStep, a.window, a.sinks);
+        // rows: keys; columns: queries
+        float ds[4][8];
+        f2 d[4][8];
+        dot_half<kLd, kLd>(d, sK, sQ, 16, 0, ry, cx);
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            f2 d[4][8];
-            dot_half<kLd, kLd>(d, sQ, sK, 16, half, ry, cx);
+        for (int j = 0; j < 8; ++j) {
+            const float base = s_lse[cx + 8 * j];
 #pragma unroll
-            for (int i4 = 0; i4 < 4; ++i4) {
-                const int i = 4 * half + i4, r = ry + 8 * i;
-                const float base = s_lse[r];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) ds[i][j] = sees(row0 + r, k0 + cx + 8 * j, a.window, a.sinks) ? exp2_approx(fmaf(sum2(d[i4][j]), a.c, -base)) : 0.f;
+            for (int i = 0; i < 4; ++i) {
+                const bool v = whole || sees(row0 + cx + 8 * j, k0 + ry + 8 * i, a.window, a.sinks);
+                ds[i][j] = v ? exp2_approx(fmaf(sum2(d[i][j]), a.c, -base)) : 0.f;
             }
-            dot_half<kLd, kLd>(d, sG, sV, 16, half, ry, cx);
+        }
+        dot_half<kLd, kLd>(d, sV, sG, 16, 0, ry, cx);
+        __syncthreads();                                  // everyone has read the values
 #pragma unroll
-            for (int i4 = 0; i4 < 4; ++i4) {
-                const int i = 4 * half + i4, r = ry + 8 * i;
-                const float D = s_D[r];
+        for (int j = 0; j < 8; ++j) {
+            const float D = s_D[cx + 8 * j];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) ds[i][j] = sees(row0 + r, k0 + cx + 8 * j, a.window, a.sinks) ? ds[i][j] * (sum2(d[i4][j]) - D) : 0.f;
+            for (int i = 0; i < 4; ++i) {
+                const bool v = whole || sees(row0 + cx + 8 * j, k0 + ry + 8 * i, a.window, a.sinks);
+                sP[(ry + 8 * i) * kLd + cx + 8 * j] = v ? ds[i][j] * (sum2(d[i][j]) - D) : 0.f;
             }
         }
         __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sP[(cx + 8 * j) * kLd + ry + 8 * i] = ds[i][j];
-        __syncthreads();
-        outer_product(acc, sP, sK, kTile, kLd, ry, cx);
+        outer_product(acc, sP, sK, kStep, kLd, ry, cx);
     }
     s_bad[tid] = 0;
     __syncthreads();
@@ -271,7 +292,7 @@ win_dq_kernel(const __grid_constant__ WinArgs a) {
         }
 }
 
-constexpr size_t kDkvSmem = 6 * kUnit * sizeof(float);
+constexpr size_t kDkvSmem = 4 * kUnit * sizeof(float);
 
 // The gradients of 64 keys and values: sums over the query rows that see them, head by head of those that share them (a fixed order).
 template <typename T>
@@ -279,67 +300,70 @@ __global__ void __launch_bounds__(kThreads)
 win_dkv_kernel(const __grid_constant__ WinArgs a) {
     pdl_sync();
     extern __shared__ float sm[];
-    __shared__ float s_D[kTile], s_lse[kTile];
+    __shared__ float s_D[kStep], s_lse[kStep];
     __shared__ int s_bad[kTile];
-    float *sK = sm, *sV = sm + kUnit, *sQ = sm + 2 * kUnit, *sG = sm + 3 * kUnit, *sP = sm + 4 * kUnit, *sS = sm + 5 * kUnit;
+    float *sK = sm, *sV = sm + kUnit, *sQ = sm + 2 * kUnit, *sG = sQ + kStep * kLd, *sP = sm + 3 * kUnit, *sS = sP + kStep * kLd;
     const int tid = threadIdx.x, ry = tid / 8, cx = tid % 8;
-    const Place pl = place_of(a, a.Hkv);
-    const int64_t koff = pl.b * a.kb + pl.h * a.kh;
+    const int tiles = (a.n + kTile - 1) / kTile;
+    const KeyItem it = key_item(a, blockIdx.x, kTile, [&](int x) { return x / tiles; }, [&](int x) { return x / a.Hkv; },
+                                [&](int x) { return x / a.parts; });
+    const int64_t koff = it.b * a.kb + it.h * a.kh;
     T *dK = (T*)a.dK + koff, *dV = (T*)a.dV + koff;
-    const int key0 = pl.row0, len = pl.len, n_end = key0 + kTile < a.n ? key0 + kTile : a.n, end = key0 + kTile < len ? key0 + kTile : len;
-    const int none = end > key0 ? end - key0 : 0;
-    zero_rows(dK + (int64_t)none * a.kn, a.kn, key0, n_end - none);
-    zero_rows(dV + (int64_t)none * a.kn, a.kn, key0, n_end - none);
-    if (end <= key0) return;
+    const int key0 = it.key0, len = it.len, n_end = key0 + kTile < a.n ? key0 + kTile : a.n, end = key0 + kTile < len ? key0 + kTile : len;
+    if (it.part <= 0) {
+        const int none = end > key0 ? end - key0 : 0;
+        zero_rows(dK + (int64_t)none * a.kn, a.kn, key0, n_end - none);
+        zero_rows(dV + (int64_t)none * a.kn, a.kn, key0, n_end - none);
+    }
+    if (it.empty()) return;
+    const int row_end = it.end(a, kTile);
     load_tile(sK, (const T*)a.K + koff, a.kn, key0, end);
     load_tile(sV, (const T*)a.V + koff, a.kn, key0, end);
     Acc ak, av;
     ak.zero();
     av.zero();
-    const int q_end = rows_end(key0, end - 1, a.window, a.sinks, len);
     for (int g = 0; g < a.G; ++g) {
-        const int h = pl.h * a.G + g;
-        const int64_t qoff = pl.b * a.qb + h * a.qh, soff = ((int64_t)pl.b * a.H + h) * a.n;
+        const int h = it.h * a.G + g;
+        const int64_t qoff = it.b * a.qb + h * a.qh, soff = ((int64_t)it.b * a.H + h) * a.n;
         const T *Q = (const T*)a.Q + qoff, *dO = (const T*)a.dO + qoff;
-        for (int i0 = key0; i0 < q_end; i0 += kTile) {
+        for (int i0 = it.begin; i0 < row_end; i0 += kStep) {
             __syncthreads();
-            load_tile(sQ, Q, a.qn, i0, len);
-            load_tile(sG, dO, a.qn, i0, len);
-            s_lse[tid] = i0 + tid < len ? -a.stat_l[soff + i0 + tid] : 0.f;
-            s_D[tid] = i0 + tid < len ? -a.stat_d[soff + i0 + tid] : 0.f;
+            load_tile<kStep>(sQ, Q, a.qn, i0, len);
+            load_tile<kStep>(sG, dO, a.qn, i0, len);
+            const int si = i0 + tid % kStep;
+            (tid < kStep ? s_lse : s_D)[tid % kStep] = si < len ? -(tid < kStep ? a.stat_l : a.stat_d)[soff + si] : 0.f;
+            cp_wait<0>();
             __syncthreads();
+            const bool whole = i0 + kStep <= len && key0 + kTile - 1 <= i0 && (i0 + kStep - 1 - key0 < a.window || key0 + kTile <= a.sinks);
             // rows: queries; columns: keys
+            f2 d[4][8];
+            float p[4][8];
+            dot_half<kLd, kLd>(d, sQ, sK, 16, 0, ry, cx);
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                f2 d[4][8];
-                float p[4][8];
-                dot_half<kLd, kLd>(d, sQ, sK, 16, half, ry, cx);
+            for (int i = 0; i < 4; ++i) {
+                const int r = ry + 8 * i;
+                const float base = s_lse[r];
 #pragma unroll
-                for (int i4 = 0; i4 < 4; ++i4) {
-                    const int r = ry + 8 * (4 * half + i4);
-                    const float base = s_lse[r];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const bool v = i0 + r < len && sees(i0 + r, key0 + cx + 8 * j, a.window, a.sinks);
-                        p[i4][j] = v ? exp2_approx(fmaf(sum2(d[i4][j]), a.c, -base)) : 0.f;
-                        sP[r * kLd + cx + 8 * j] = p[i4][j];
-                    }
+                for (int j = 0; j < 8; ++j) {
+                    const bool v = whole || (i0 + r < len && sees(i0 + r, key0 + cx + 8 * j, a.window, a.sinks));
+                    p[i][j] = v ? exp2_approx(fmaf(sum2(d[i][j]), a.c, -base)) : 0.f;
+                    sP[r * kLd + cx + 8 * j] = p[i][j];
                 }
-                dot_half<kLd, kLd>(d, sG, sV, 16, half, ry, cx);
+            }
+            dot_half<kLd, kLd>(d, sG, sV, 16, 0, ry, cx);
 #pragma unroll
-                for (int i4 = 0; i4 < 4; ++i4) {
-                    const int r = ry + 8 * (4 * half + i4);
-                    const float D = s_D[r];
+            for (int i = 0; i < 4; ++i) {
+                const int r = ry + 8 * i;
+                const float D = s_D[r];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const bool v = i0 + r < len && sees(i0 + r, key0 + cx + 8 * j, a.window, a.sinks);
-                        sS[r * kLd + cx + 8 * j] = v ? p[i4][j] * (sum2(d[i4][j]) - D) : 0.f;
-                    }
+                for (int j = 0; j < 8; ++j) {
+                    const bool v = whole || (i0 + r < len && sees(i0 + r, key0 + cx + 8 * j, a.window, a.sinks));
+                    sS[r * kLd + cx + 8 * j] = v ? p[i][j] * (sum2(d[i][j]) - D) : 0.f;
                 }
             }
             __syncthreads();
-            outer_product(av, sP, sG, kTile, kLd, ry, cx);
-            outer_product(ak, sS, sQ, kTile, kLd, ry, cx);
+            outer_product(av, sP, sG, kStep, kLd, ry, cx);
+            outer_product(ak, sS, sQ, kStep, kLd, ry, cx);
         }
     }
     s_bad[tid] = 0;
@@ -349,19 +373,49 @@ win_dkv_kernel(const __grid_constant__ WinArgs a) {
         const int r = out_row(ry, i);
         float k[8], v[8];
         const bool fk = row_out(ak, i, a.scale, k), fv = row_out(av, i, 1.f, v), fine = fk && fv;
-        if (key0 + r < end && fine) {
-            store_row(dK + (int64_t)(key0 + r) * a.kn, cx, k);
-            store_row(dV + (int64_t)(key0 + r) * a.kn, cx, v);
+        // (a part's sums stay as they are: each of its pairs counts)
+        if (key0 + r < end && (fine || it.part > 0)) {
+            if (it.part <= 0) {
+                store_row(dK + (int64_t)(key0 + r) * a.kn, cx, k);
+                store_row(dV + (int64_t)(key0 + r) * a.kn, cx, v);
+            }
+            if (it.part >= 0 && r < a.sinks) {
+                store_row(partial_row(a, it.b, it.h, it.part, 0, r), cx, k);
+                store_row(partial_row(a, it.b, it.h, it.part, 1, r), cx, v);
+            }
         }
-        if (cx == 0 && !fine) s_bad[r] = 1;
+        if (cx == 0 && !fine && it.part <= 0) s_bad[r] = 1;
     }
     __syncthreads();
     for (int r = tid / 32; key0 + r < end && r < kTile; r += kThreads / 32)
         if (s_bad[r]) {
-            const KeyRow k = redo_dkv_row<T>(a, pl.b, pl.h, key0 + r, len);
-            st2(dK + (int64_t)(key0 + r) * a.kn + 2 * (tid % 32), k.dk);
-            st2(dV + (int64_t)(key0 + r) * a.kn + 2 * (tid % 32), k.dv);
+            const int c = 2 * (tid % 32);
+            const bool sum = it.part == 0 && r < a.sinks;
+            const KeyRow k = redo_dkv_row<T>(a, it.b, it.h, key0 + r, len, sum ? row_end : len);
+            st2(dK + (int64_t)(key0 + r) * a.kn + c, k.dk);
+            st2(dV + (int64_t)(key0 + r) * a.kn + c, k.dv);
+            if (sum) {
+                st2(partial_row(a, it.b, it.h, 0, 0, r) + c, k.dk);
+                st2(partial_row(a, it.b, it.h, 0, 1, r) + c, k.dv);
+            }
         }
+}
+
+// The sinks' gradients from their parts.
+template <typename T>
+__global__ void __launch_bounds__(256)
+win_sink_sum_kernel(const __grid_constant__ WinArgs a) {
+    pdl_sync();
+    const int b = blockIdx.x / a.Hkv, hk = blockIdx.x % a.Hkv, len = length_of(a, b), rows = a.sinks < len ? a.sinks : len;
+    const int64_t koff = b * a.kb + hk * a.kh;
+    const int e = blockIdx.y * 256 + threadIdx.x;
+    if (e < rows * 128) {
+        const int which = e / (rows * 64), j = e / 64 % rows, c = e % 64;
+        float t = partial_row(a, b, hk, 0, which, j)[c];
+#pragma unroll 8
+        for (int q = 0; q < a.parts && a.split_row + q * a.part_rows < len; ++q) t += partial_row(a, b, hk, q + 1, which, j)[c];
+        stf((T*)(which ? a.dV : a.dK) + koff + (int64_t)j * a.kn + c, t);
+    }
 }
 
 template <typename Kern>
@@ -382,7 +436,15 @@ template <typename T>
 cudaError_t cc_window_bwd(const WinArgs& a, cudaStream_t s) {
     const unsigned tiles = (unsigned)((a.n + kTile - 1) / kTile);
     const cudaError_t e = launch_rows("win_dq_kernel", win_dq_kernel<T>, kDqSmem, tiles * a.B * a.H, a, s);
-    return e != cudaSuccess ? e : launch_rows("win_dkv_kernel", win_dkv_kernel<T>, kDkvSmem, tiles * a.B * a.Hkv, a, s);
+    return e != cudaSuccess ? e : launch_rows("win_dkv_kernel", win_dkv_kernel<T>, kDkvSmem, (tiles + a.parts) * a.B * a.Hkv, a, s);
+}
+cudaError_t sink_sum(const WinArgs& a, bool half, cudaStream_t s) {
+    if (a.parts == 0) return cudaSuccess;
+    prof_begin("win_sink_sum_kernel", s);
+    if (half) launch_pdl(win_sink_sum_kernel<bf16>, dim3(a.B * a.Hkv, (a.sinks + 1) / 2), dim3(256), 0, s, a);
+    else launch_pdl(win_sink_sum_kernel<float>, dim3(a.B * a.Hkv, (a.sinks + 1) / 2), dim3(256), 0, s, a);
+    prof_end(s);
+    return cudaGetLastError();
 }
 
 }  // namespace
@@ -425,6 +487,20 @@ int check_rows(const psk_window_shape* sh) {
     st = check_strides(sh->B, sh->H, sh->n, sh->q_stride_b, sh->q_stride_h, sh->q_stride_n, esz);
     return st != PSK_OK ? st : check_strides(sh->B, sh->Hkv, sh->n, sh->kv_stride_b, sh->kv_stride_h, sh->kv_stride_n, esz);
 }
+void plan_parts(WinArgs& a, int tile) {
+    a.parts = a.part_rows = a.split_row = 0;
+    if (a.sinks == 0 || a.sinks > tile) return;
+    const int64_t split = ((int64_t)tile + a.window - 1 + 63) / 64 * 64;               // rows before it see more than the sinks
+    if (split >= a.n) return;
+    const int64_t base = split / 64, rest = (a.n - split + 63) / 64;                   // steps of 64 rows
+    if (rest <= base) return;
+    // parts no longer than the other tiles' work, and no more of them than keep the GPU busy
+    const int64_t keyheads = (int64_t)a.B * a.Hkv, most = 1024 / keyheads + 1, want = (rest + (base > 8 ? base : 8) - 1) / (base > 8 ? base : 8);
+    const int64_t parts = want < most ? want : most;
+    a.split_row = (int)split;
+    a.part_rows = (int)((rest + parts - 1) / parts * 64);
+    a.parts = (int)((a.n - split + a.part_rows - 1) / a.part_rows);
+}
 static bool on_tensor_cores(const psk_window_shape* sh) { return sh->dtype == PSK_BF16 && sh->path != PSK_PATH_CUDA_CORES; }
 WinArgs args_of(const psk_window_shape* sh) {
     WinArgs a{};
@@ -447,7 +523,15 @@ extern "C" {
 
 size_t psk_window_workspace_bytes(const psk_window_shape* shape, int for_backward) {
     if (check_rows(shape) != PSK_OK) return 0;
-    return kStatusBytes + (for_backward ? 2 * align_up((size_t)shape->B * shape->H * shape->n * sizeof(float)) : 0);
+    if (!for_backward) return kStatusBytes;
+    WinArgs a = args_of(shape);
+    size_t parts = 0;                                     // (enough for either path)
+    for (int tile = kTile; tile <= 128; tile += 64) {
+        plan_parts(a, tile);
+        const size_t bytes = a.parts > 0 ? align_up((size_t)a.B * a.Hkv * (a.parts + 1) * 2 * a.sinks * 64 * sizeof(float)) : 0;
+        if (bytes > parts) parts = bytes;
+    }
+    return kStatusBytes + 2 * align_up((size_t)a.B * a.H * a.n * sizeof(float)) + parts;
 }
 
 int psk_window_attn_fwd(const psk_window_shape* shape, const void* Q, const void* K, const void* V, const int32_t* lengths, void* O, float* lse,
@@ -487,6 +571,8 @@ int psk_window_attn_bwd(const psk_window_shape* shape, const void* Q, const void
     a.Q = Q; a.K = K; a.V = V; a.O = O; a.lse_in = lse; a.dO = dO; a.dQ = dQ; a.dK = dK; a.dV = dV; a.lengths = lengths;
     a.stat_l = reinterpret_cast<float*>(static_cast<char*>(workspace) + kStatusBytes);
     a.stat_d = a.stat_l + align_up((size_t)a.B * a.H * a.n * sizeof(float)) / sizeof(float);
+    a.partial = a.stat_d + align_up((size_t)a.B * a.H * a.n * sizeof(float)) / sizeof(float);
+    plan_parts(a, on_tensor_cores(shape) ? 128 : kTile);
     int* status = static_cast<int*>(workspace);
     cudaError_t e;
     if (on_tensor_cores(shape)) {
@@ -495,6 +581,7 @@ int psk_window_attn_bwd(const psk_window_shape* shape, const void* Q, const void
         a.status = status;
         e = shape->dtype == PSK_F32 ? cc_window_bwd<float>(a, s) : cc_window_bwd<bf16>(a, s);
     }
+    if (e == cudaSuccess) e = sink_sum(a, shape->dtype == PSK_BF16, s);
     return e == cudaSuccess ? PSK_OK : PSK_ERR_CUDA;
 }
 

@@ -23,7 +23,15 @@ struct WinArgs {
     int B, H, Hkv, G, n, window, sinks;
     float scale, c;                   // c = scale log2(e)
     int64_t qb, qh, qn, kb, kh, kn;   // element strides of the query-side and of the key-side tensors
+    // Key side: the tile with the sinks is seen by every row of its sequence, any other by a window's.  Where that makes it much longer, the rows
+    // from `split_row` on are left to `parts` items of `part_rows` rows each, and the sinks' gradients are added up from
+    // `partial` [B Hkv][parts + 1][dK, dV][sinks][64] in a fixed order (part 0: the rows before split_row).  parts = 0: nothing of that.
+    int parts, part_rows, split_row;
+    float* partial;
 };
+__device__ __forceinline__ float* partial_row(const WinArgs& a, int b, int hk, int part, int which, int j) {
+    return a.partial + ((((int64_t)b * a.Hkv + hk) * (a.parts + 1) + part) * 2 + which) * a.sinks * 64 + (int64_t)j * 64;
+}
 
 __device__ __forceinline__ int length_of(const WinArgs& a, int b) {
     if (a.lengths == nullptr) return a.n;
@@ -102,16 +110,16 @@ __device__ __noinline__ float2 redo_dq_row(const T* q, const T* dO, const T* K, 
     return make_float2(acc.x * scale, acc.y * scale);
 }
 
-// row j of key head hk of sequence b: (dk, dv)
+// row j of key head hk of sequence b: (dk, dv), from the query rows before `stop`
 struct KeyRow { float2 dk, dv; };
 template <typename T>
-__device__ __noinline__ KeyRow redo_dkv_row(const WinArgs& a, int b, int hk, int j, int len) {
+__device__ __noinline__ KeyRow redo_dkv_row(const WinArgs& a, int b, int hk, int j, int len, int stop) {
     const int l2 = 2 * (threadIdx.x % 32);
     const int64_t krow = b * a.kb + hk * a.kh + j * a.kn + l2;
     const float2 k = ld2((const T*)a.K + krow), v = ld2((const T*)a.V + krow);
     KeyRow r{make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
     const int64_t past = (int64_t)j + a.window;
-    const int end = (j < a.sinks || past > len) ? len : (int)past;
+    const int most = len < stop ? len : stop, end = (j < a.sinks || past > most) ? most : (int)past;
     for (int g = 0; g < a.G; ++g) {
         const int h = hk * a.G + g;
         for (int i = j; i < end; ++i) {
@@ -147,10 +155,47 @@ __device__ __forceinline__ int rows_end(int key0, int key1, int window, int sink
     return (key0 < sinks || past > len) ? len : (int)past;
 }
 
+// The work of a key-side item: the keys key0 .. of a head, the query rows from `begin` on and before `stop`, and which part of the sinks' sums
+// they make (-1: those are not split).  Items before the tiles' are the parts of the sinks' tile.
+struct KeyItem {
+    int b, h, key0, len, begin, stop, part;
+    __device__ __forceinline__ bool empty() const { return begin >= stop; }
+    // one past its last row (not kept: a register of the loop over the rows)
+    __device__ __forceinline__ int end(const WinArgs& a, int tile) const {
+        const int e = rows_end(key0, (key0 + tile < len ? key0 + tile : len) - 1, a.window, a.sinks, len);
+        return e < stop ? e : stop;
+    }
+};
+template <typename D1, typename D2, typename D3>
+__device__ __forceinline__ KeyItem key_item(const WinArgs& a, int index, int tile, const D1& by_tiles, const D2& by_heads, const D3& by_parts) {
+    KeyItem k;
+    const int first = a.parts * a.B * a.Hkv;              // (the parts first: they are the longer ones)
+    int bh, q = -1;
+    if (index >= first) { bh = by_tiles(index - first); k.key0 = (index - first - bh * ((a.n + tile - 1) / tile)) * tile; }
+    else { bh = by_parts(index); q = index - bh * a.parts; k.key0 = 0; }
+    k.b = by_heads(bh);
+    k.h = bh - k.b * a.Hkv;
+    k.len = length_of(a, k.b);
+    k.begin = k.key0;
+    k.stop = k.len;
+    k.part = -1;
+    if (a.parts > 0 && k.key0 == 0) {
+        if (q < 0) {
+            k.stop = k.len < a.split_row ? k.len : a.split_row;
+        } else {
+            k.begin = a.split_row + q * a.part_rows;
+            k.stop = k.len - k.begin < a.part_rows ? k.len : k.begin + a.part_rows;
+        }
+        k.part = q + 1;
+    }
+    return k;
+}
+
 // host: argument checks and what the kernels take (psk_window.cu)
 int check_common(const psk_window_shape* sh);         // all but n and the strides
 int check_rows(const psk_window_shape* sh);
 WinArgs args_of(const psk_window_shape* sh);
+void plan_parts(WinArgs& a, int tile);                // fills parts, part_rows, split_row
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // tensor cores (psk_window_tc.cu): bf16

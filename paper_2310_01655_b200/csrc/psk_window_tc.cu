@@ -23,7 +23,7 @@ constexpr int kRows = 128;
 // Items
 // ---------------------------------------------------------------------------
 struct Item { int b, h, row0, len; };
-struct ItemMap { FastDiv tiles, heads; };
+struct ItemMap { FastDiv tiles, heads, parts; };
 __device__ __forceinline__ Item item_of(const WinArgs& a, const ItemMap& m, int index) {
     const int bh = m.tiles.div(index);
     Item p;
@@ -123,6 +123,18 @@ __device__ __forceinline__ bool stage_half(uint8_t* st, int row, int half, uint3
 __device__ __forceinline__ bool stage_row(uint8_t* st, int row, uint32_t taddr, float f, bool live) {
     const bool a = stage_half(st, row, 0, taddr, f, live), b = stage_half(st, row, 1, taddr, f, live);
     return a && b;
+}
+// A row of 64 values times f into memory as fp32 (where `live`), for sums over parts.
+__device__ __forceinline__ void store_partial(float* dst, uint32_t taddr, float f, bool live) {
+#pragma unroll 1
+    for (int q = 0; q < 64; q += 16) {
+        Cols<16> o;
+        o.load(taddr + q);
+        tmem_ld_wait();
+#pragma unroll
+        for (int j = 0; j < 16; j += 4)
+            if (live) *reinterpret_cast<float4*>(dst + q + j) = make_float4(o[j] * f, o[j + 1] * f, o[j + 2] * f, o[j + 3] * f);
+    }
 }
 // two values of a staged row, by each lane of a warp (whose columns lie in that half)
 __device__ __forceinline__ void stage_pair(uint8_t* st, int row, float2 v, int half = -1) {
@@ -728,6 +740,8 @@ struct Dkv {
     static constexpr uint32_t kTmem = 512, cDk = 0, cDv = 64, cS = 128;        // cS + 128 warpgroup: S (p), dP (ds)
 };
 
+// PARTS: there are items that are parts of the sinks' tiles (the code for them costs others 4 %: 699 against 674 us on 8192 rows of 16 x 12 heads)
+template <bool PARTS>
 __global__ void __launch_bounds__(Dkv::kThreads, 1)
 tc_win_dkv_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV, const __grid_constant__ CUtensorMap mapQ,
                   const __grid_constant__ CUtensorMap mapG, const __grid_constant__ CUtensorMap mapDk, const __grid_constant__ CUtensorMap mapDv,
@@ -755,11 +769,16 @@ tc_win_dkv_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constan
     __syncthreads();
     tc_fence_after();
     const uint32_t tm = tm_slot;
-    // steps per query head of an item: tiles of 64 rows from the first key's on
-    auto tiles_of = [&](const Item& p) {
-        const int key1 = (p.row0 + kRows < p.len ? p.row0 + kRows : p.len) - 1;
-        return (rows_end(p.row0, key1, a.window, a.sinks, p.len) - p.row0 + 63) / 64;
+    auto item = [&](int index) {
+        if constexpr (PARTS) {
+            return key_item(a, index, kRows, [&](int x) { return (int)map.tiles.div(x); }, [&](int x) { return (int)map.heads.div(x); },
+                            [&](int x) { return (int)map.parts.div(x); });
+        } else {
+            const Item q = item_of(a, map, index);
+            return KeyItem{q.b, q.h, q.row0, q.len, q.row0, q.len, -1};
+        }
     };
+    auto tiles_of = [&](const KeyItem& p) { return (p.end(a, kRows) - p.begin + 63) / 64; };       // steps per query head
     if (warp == Dkv::kLoad) {
         bool ok = true;
         int t = 0, items = 0;
@@ -767,8 +786,8 @@ tc_win_dkv_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constan
             ok = __all_sync(0xffffffffu, sched_free(sched, it, status));
             if (!ok) break;
             if (elect_one()) sched_ask(sched, it);
-            const Item p = item_of(a, map, index);
-            if (p.row0 < p.len) {
+            const KeyItem p = item(index);
+            if (!p.empty()) {
                 const int kv = items & 1, tiles = tiles_of(p), steps = tiles * a.G;
                 if (items >= 2) ok = mbar_wait(&free_kv[kv], (items / 2 - 1) & 1, status, kErrMma);
                 ok = __all_sync(0xffffffffu, ok);
@@ -776,12 +795,12 @@ tc_win_dkv_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constan
                 ++items;
                 if (elect_one()) {
                     mbar_expect_tx(&bar_kv[kv], 32768);
-                    tma_load_4d(smem + Dkv::KV + kv * 32768, &mapK, 0, p.row0, p.h, p.b, &bar_kv[kv]);
-                    tma_load_4d(smem + Dkv::KV + kv * 32768 + 16384, &mapV, 0, p.row0, p.h, p.b, &bar_kv[kv]);
+                    tma_load_4d(smem + Dkv::KV + kv * 32768, &mapK, 0, p.key0, p.h, p.b, &bar_kv[kv]);
+                    tma_load_4d(smem + Dkv::KV + kv * 32768 + 16384, &mapV, 0, p.key0, p.h, p.b, &bar_kv[kv]);
                 }
-                for (int x = 0, h = p.h * a.G, i0 = p.row0; x < steps; ++x, ++t, i0 += 64) {
+                for (int x = 0, h = p.h * a.G, i0 = p.begin; x < steps; ++x, ++t, i0 += 64) {
                     const int s = t % Dkv::kStages;
-                    if (i0 - p.row0 == tiles * 64) { i0 = p.row0; ++h; }
+                    if (i0 - p.begin == tiles * 64) { i0 = p.begin; ++h; }
                     if (t >= Dkv::kStages) ok = mbar_wait(&free_qg[s], (t / Dkv::kStages - 1) & 1, status, kErrMma);
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
@@ -842,9 +861,9 @@ tc_win_dkv_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constan
                 if (last) umma_commit(&bar_fin[(w.started - 1) & 3]);
             };
             for (int it = 0, index = blockIdx.x; index >= 0 && ok; ++it) {
-                const Item p = item_of(a, map, index);
+                const KeyItem p = item(index);
                 const int begun = w.t;
-                if (p.row0 < p.len) {
+                if (!p.empty()) {
                     const int kv = items & 1, steps = tiles_of(p) * a.G;
                     ok = mbar_wait(&bar_kv[kv], (items / 2) & 1, status, kErrTma);
                     ++items;
@@ -878,16 +897,16 @@ tc_win_dkv_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constan
         bool ok = true;
         int t = group, t0 = 0, items = 0;
         for (int it = 0, index = blockIdx.x; index >= 0; ++it) {
-            const Item p = item_of(a, map, index);
-            const int j = p.row0 + row, j_first = p.row0 + warp % 4 * 32;
-            if (p.row0 < p.len) {
+            const KeyItem p = item(index);
+            const int j = p.key0 + row, j_first = p.key0 + warp % 4 * 32;
+            if (!p.empty()) {
                 const int rows = tiles_of(p) * 64, end = t0 + rows / 64 * a.G;
                 const int64_t past = (int64_t)j + a.window;
                 const int last_row = ((j < a.sinks || past > p.len) ? p.len : (int)past) - 1;      // the last query row that sees this key
-                int off = (t - t0) * 64;                  // of the step's first row from the first key
+                int off = (t - t0) * 64;                  // of the step's first row from the item's
                 for (; t < end; t += kGroups, off += kGroups * 64) {
                     while (off >= rows) off -= rows;      // (the next head's rows)
-                    const int i0 = p.row0 + off, stage = t % Dkv::kStages;
+                    const int i0 = p.begin + off, stage = t % Dkv::kStages;
                     ok = mbar_wait(&bar_qg[stage], (t / Dkv::kStages) & 1, status, kErrTma) && ok;     // (the rows' statistics)
                     ok = mbar_wait(&bar_s[group], (t / kGroups) & 1, status, kErrMma) && ok;
                     tc_fence_after();
@@ -931,24 +950,36 @@ tc_win_dkv_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constan
                     ok = mbar_wait(&bar_fin[items & 3], (items / 4) & 1, status, kErrMma) && ok;
                     tc_fence_after();
                     bar_sync(1 + group, kRows);
-                    const bool live = j < p.len, fine = stage_row(st, row, lane_tm + (has_k ? Dkv::cDk : Dkv::cDv), has_k ? a.scale : 1.f, live);
-                    tc_fence_before();
-                    unsigned bad = __ballot_sync(0xffffffffu, ok && !fine && live);
-                    if (lane == 0) mbar_arrive(&bar_acc);
-                    while (bad != 0) {
-                        const int k = __ffs(bad) - 1;
-                        bad &= bad - 1;
-                        const KeyRow r = redo_dkv_row<bf16>(a, p.b, p.h, j_first + k, p.len);
-                        stage_pair(st, warp % 4 * 32 + k, has_k ? r.dk : r.dv);
+                    const bool live = j < p.len, sum = PARTS && p.part >= 0 && row < a.sinks;      // sum: this row's gradients are added up from parts
+                    const uint32_t from = lane_tm + (has_k ? Dkv::cDk : Dkv::cDv);
+                    const float f = has_k ? a.scale : 1.f;
+                    if (PARTS && __any_sync(0xffffffffu, sum)) store_partial(partial_row(a, p.b, p.h, p.part, has_k ? 0 : 1, row), from, f, ok && sum && live);
+                    if (PARTS && p.part > 0) {
+                        tc_fence_before();
+                        if (lane == 0) mbar_arrive(&bar_acc);
+                    } else {
+                        const bool fine = stage_row(st, row, from, f, live);
+                        tc_fence_before();
+                        unsigned bad = __ballot_sync(0xffffffffu, ok && !fine && live);
+                        if (lane == 0) mbar_arrive(&bar_acc);
+                        if (PARTS) __syncwarp();          // (the partial row is written over below)
+                        while (bad != 0) {
+                            const int k = __ffs(bad) - 1, r = warp % 4 * 32 + k;
+                            bad &= bad - 1;
+                            const bool part = PARTS && p.part == 0 && r < a.sinks;
+                            const KeyRow key = redo_dkv_row<bf16>(a, p.b, p.h, j_first + k, p.len, part ? p.stop : p.len);
+                            stage_pair(st, r, has_k ? key.dk : key.dv);
+                            if (part) st2(partial_row(a, p.b, p.h, 0, has_k ? 0 : 1, r) + 2 * lane, has_k ? key.dk : key.dv);
+                        }
+                        fence_proxy_async_smem();
+                        bar_sync(1 + group, kRows);
+                        if (row == 0 && !cta_gave_up()) { tma_store_4d(has_k ? &mapDk : &mapDv, st, 0, p.key0, p.h, p.b); bulk_commit(); }
                     }
-                    fence_proxy_async_smem();
-                    bar_sync(1 + group, kRows);
-                    if (row == 0 && !cta_gave_up()) { tma_store_4d(has_k ? &mapDk : &mapDv, st, 0, p.row0, p.h, p.b); bulk_commit(); }
                 }
                 t0 = end;
                 ++items;
-            } else if (group < 2) {
-                zero_tile<kRows>((bf16*)(group == 0 ? a.dK : a.dV) + p.b * a.kb + p.h * a.kh, a.kn, p.row0, a.n, row);
+            } else if (group < 2 && p.part <= 0) {
+                zero_tile<kRows>((bf16*)(group == 0 ? a.dK : a.dV) + p.b * a.kb + p.h * a.kh, a.kn, p.key0, a.n, row);
             }
             index = sched_next(sched, it, status);
             if (bar_any(1 + group, kRows, index < 0)) index = -1;            // (a whole warpgroup or none of it: it shares barriers)
@@ -965,6 +996,7 @@ ItemMap item_map(const WinArgs& a, int heads) {
     ItemMap m;
     m.tiles.set((uint32_t)((a.n + kRows - 1) / kRows));
     m.heads.set((uint32_t)heads);
+    m.parts.set((uint32_t)(a.parts > 0 ? a.parts : 1));
     return m;
 }
 bool map_q(const WinArgs& a, CUtensorMap* m, const void* p, int rows) { return tc_map_rows(m, p, a.B, a.H, a.n, a.qb, a.qh, a.qn, rows); }
@@ -998,9 +1030,10 @@ cudaError_t tc_window_bwd(const WinArgs& a, int* status, cudaStream_t s) {
     if (!map_k(a, &mK, a.K, 128) || !map_k(a, &mV, a.V, 128) || !map_q(a, &mQ, a.Q, 64) || !map_q(a, &mG, a.dO, 64) || !map_k(a, &mDk, a.dK, 128) ||
         !map_k(a, &mDv, a.dV, 128))
         return cudaErrorInvalidValue;
-    PSK_TRY(set_smem(tc_win_dkv_kernel, Dkv::bytes));
+    const auto dkv = a.parts > 0 ? tc_win_dkv_kernel<true> : tc_win_dkv_kernel<false>;
+    PSK_TRY(set_smem(dkv, Dkv::bytes));
     prof_begin("tc_win_dkv_kernel", s);
-    launch_pdl(tc_win_dkv_kernel, dim3(tiles * a.B * a.Hkv), dim3(Dkv::kThreads), Dkv::bytes, s, mK, mV, mQ, mG, mDk, mDv, a, item_map(a, a.Hkv), status);
+    launch_pdl(dkv, dim3((tiles + a.parts) * a.B * a.Hkv), dim3(Dkv::kThreads), Dkv::bytes, s, mK, mV, mQ, mG, mDk, mDv, a, item_map(a, a.Hkv), status);
     prof_end(s);
     return cudaGetLastError();
 }

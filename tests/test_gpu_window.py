@@ -133,6 +133,32 @@ def test_sequences_of_all_lengths(dtype, path, window, sinks):
 
 
 @pytest.mark.parametrize("dtype,path", PATHS)
+@pytest.mark.parametrize("B,H,Hkv,n,window,sinks,lengths", [
+    (1, 1, 1, 1400, 40, 4, None), (2, 4, 2, 1111, 100, 64, [1111, 300]), (1, 2, 1, 1500, 1, 1, None), (3, 2, 2, 900, 64, 100, [0, 150, 900]),
+    (2, 3, 1, 2050, 129, 128, [2049, 2050]), (1, 2, 2, 700, 30, 200, None), (4, 1, 1, 1000, 65, 2, [1, 2, 320, 321])])
+def test_sinks_of_long_sequences(dtype, path, B, H, Hkv, n, window, sinks, lengths):
+    """The sinks are seen by every row: their gradients may be added up from several parts."""
+    Q, K, V, dO = make(dtype, B, H, Hkv, n, seed=n)
+    lens = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    out = run(Q, K, V, dO, window, sinks, path=path, lengths=lens)
+    check_heads(dtype, Q, K, V, dO, out, window, sinks, lengths=lengths, heads=[(b, Hkv - 1) for b in range(B)])
+    for b in range(B if lengths else 0):
+        assert all(x[b, :, lengths[b]:].eq(0).all() for x in out[2:])
+    for x, y in zip(out, run(Q, K, V, dO, window, sinks, path=path, lengths=lens)):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype,path", PATHS)
+@pytest.mark.parametrize("row", [10, 700])
+def test_sinks_of_long_sequences_with_infinities(dtype, path, row):
+    """A row of dO that is infinite in one column, among the rows of the sinks' tile or of a part: the sinks' gradients are what the sums say."""
+    Q, K, V, dO = make(dtype, 1, 2, 1, 1200, seed=3)
+    dO[0, 1, row, 5] = float("inf")
+    out = run(Q, K, V, dO, 50, 3, path=path)
+    check_heads(dtype, Q, K, V, dO, out, 50, 3)
+
+
+@pytest.mark.parametrize("dtype,path", PATHS)
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 @pytest.mark.parametrize("window,sinks", [(70, 0), (200, 3), (2000, 0)])
 def test_masked_infinities_and_nans(dtype, path, bad, window, sinks):
