@@ -330,8 +330,9 @@ int psk_window_attn_bwd(const psk_window_shape* shape, const void* Q, const void
  * k, v [B, Hkv, h] into the position's slot and attends with q [B, H, h] over the slots that positions 0 .. t have written:
  * o [B, H, h] is row t of psk_window_attn_fwd when the cache holds the positions before t.  All contiguous DEVICE
  * arrays of the shape's dtype.  A negative position marks an idle place: o = 0, its cache is not touched.  Positions are
- * counted from the sequence's start and go on past the window, to 2^31 - 1.  Of the shape n and the strides are not read.  CUDA-core
- * kernel, fp32 arithmetic, for either dtype; no workspace, one launch. */
+ * counted from the sequence's start and go on past the window, to 2^31 - 1.  Of the shape n and the strides are not read.  fp32: CUDA
+ * cores.  bf16: warp matrix instructions with fp32 accumulation, the weights as two bf16 summands each (to 2^-17).  fp32 softmax; no
+ * workspace, one launch; the same bits every time. */
 size_t psk_window_cache_bytes(const psk_window_shape* shape);
 int psk_window_cache_fill(const psk_window_shape* shape, const void* K, const void* V, const int32_t* lengths, void* Kc, void* Vc,
                           void* stream);

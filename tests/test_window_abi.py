@@ -51,7 +51,7 @@ def test_layer_norm(L, field, value, code):
 def test_layer_norm_pointers(L):
     s = norm()
     need = L.psk_layer_norm_workspace_bytes(byref(s))
-    assert need >= 4 * 12 * 9 * 2 * 64 * 4
+    assert need >= 2 * 64 * 4                 # one row of both sums at least
     assert L.psk_layer_norm_fwd(None, FAKE, FAKE, FAKE, FAKE, None) == -1
     assert L.psk_layer_norm_fwd(byref(s), None, FAKE, FAKE, FAKE, None) == -1
     assert L.psk_layer_norm_fwd(byref(s), FAKE, FAKE, FAKE, None, None) == -1
