@@ -20,7 +20,7 @@ using namespace cc;
 constexpr int kTile = 64, kThreads = 64;
 
 // ROWS rows x 64 columns from row r0 into [ROWS][kLd] fp32, zeros from row `end` on.  fp32: asynchronous copies, all on their way at once (forward
-// of 24 heads x 2048 rows, window 256: 190 us; through registers, in batches of four, 215); cp_wait<> before the barrier in front of their use.
+// of 24 heads x 2048 rows, window 256: 198 us; through registers, in batches of four, 215 with 190 at the time); cp_wait<> before the barrier in front of their use.
 template <int ROWS = kTile, typename T>
 __device__ __forceinline__ void load_tile(float* dst, const T* src, int64_t stride, int r0, int end) {
     constexpr int V = 16 / sizeof(T), PerRow = 64 / V;
@@ -89,6 +89,19 @@ __device__ __forceinline__ Place place_of(const WinArgs& a, int heads) {
     p.row0 = (int)(blockIdx.x % tiles) * kTile;
     p.len = length_of(a, p.b);
     return p;
+}
+
+// (on its own: what it needs is worked out again, not kept in registers over the forward's loop)
+template <typename T>
+__device__ __noinline__ void redo_out_rows(const WinArgs& a, const int* bad) {
+    const Place z = place_of(a, a.H);
+    const int64_t at = z.b * a.qb + z.h * a.qh, from = z.b * a.kb + z.h / a.G * a.kh;
+    const T *K = (const T*)a.K + from, *V = (const T*)a.V + from;
+    for (int r = threadIdx.x / 32; r < kTile && z.row0 + r < z.len; r += kThreads / 32)
+        if (bad[r] && row_tainted(K, V, a.kn, z.row0 + r, a.window, a.sinks, z.len)) {
+            const int64_t row = at + (z.row0 + r) * a.qn;
+            st2((T*)a.out + row + 2 * (threadIdx.x % 32), redo_out_row((const T*)a.Q + row, K, V, a.kn, z.row0 + r, a.window, a.sinks, a.c));
+        }
 }
 
 constexpr size_t kFwdSmem = 4 * kUnit * sizeof(float);
@@ -188,15 +201,14 @@ win_fwd_kernel(const __grid_constant__ WinArgs a) {
     for (int i = 0; i < 8; ++i) {
         const int r = out_row(ry, i);
         float o[8];
-        const bool fine = row_out(acc, i, s_inv[r], o) && !s_bad[r];
+        // (where the statistics are not finite, neither is the row: NaN)
+        const bool fine = row_out(acc, i, s_inv[r], o) || s_bad[r];
         __syncwarp();
-        if (row0 + r < end && fine) store_row(O + (int64_t)(row0 + r) * a.qn, cx, o);
-        if (cx == 0 && !fine) s_bad[r] = 1;
+        if (row0 + r < end) store_row(O + (int64_t)(row0 + r) * a.qn, cx, o);
+        if (cx == 0) s_bad[r] = !fine;
     }
     __syncthreads();
-    for (int r = tid / 32; row0 + r < end && r < kTile; r += kThreads / 32)
-        if (s_bad[r]) st2(O + (int64_t)(row0 + r) * a.qn + 2 * (tid % 32),
-                          redo_out_row(Q + (int64_t)(row0 + r) * a.qn, K, V, a.kn, row0 + r, a.window, a.sinks, a.c, lse + row0 + r));
+    redo_out_rows<T>(a, s_bad);
 }
 
 // Keys (query side) or query rows (key side) of a step of the backward: with 32 four CTAs (three) fit into an SM, with 64 three (two):
@@ -280,13 +292,13 @@ win_dq_kernel(const __grid_constant__ WinArgs a) {
     for (int i = 0; i < 8; ++i) {
         const int r = out_row(ry, i);
         float o[8];
-        const bool fine = row_out(acc, i, a.scale, o);
-        if (row0 + r < end && fine) store_row(dQ + (int64_t)(row0 + r) * a.qn, cx, o);
+        const bool nan = s_lse[r] != s_lse[r] || s_D[r] != s_D[r], fine = row_out(acc, i, a.scale, o) || nan;      // (nan: then so is the row)
+        if (row0 + r < end) store_row(dQ + (int64_t)(row0 + r) * a.qn, cx, o);
         if (cx == 0 && !fine) s_bad[r] = 1;
     }
     __syncthreads();
     for (int r = tid / 32; row0 + r < end && r < kTile; r += kThreads / 32)
-        if (s_bad[r]) {
+        if (s_bad[r] && row_tainted(K, V, a.kn, row0 + r, a.window, a.sinks, len)) {
             const int64_t at = (int64_t)(row0 + r) * a.qn;
             st2(dQ + at + 2 * (tid % 32), redo_dq_row(Q + at, dO + at, K, V, a.kn, row0 + r, a.window, a.sinks, a.c, a.scale, make_float2(s_lse[r], s_D[r])));
         }
@@ -374,7 +386,7 @@ win_dkv_kernel(const __grid_constant__ WinArgs a) {
         float k[8], v[8];
         const bool fk = row_out(ak, i, a.scale, k), fv = row_out(av, i, 1.f, v), fine = fk && fv;
         // (a part's sums stay as they are: each of its pairs counts)
-        if (key0 + r < end && (fine || it.part > 0)) {
+        if (key0 + r < end) {
             if (it.part <= 0) {
                 store_row(dK + (int64_t)(key0 + r) * a.kn, cx, k);
                 store_row(dV + (int64_t)(key0 + r) * a.kn, cx, v);
@@ -388,7 +400,7 @@ win_dkv_kernel(const __grid_constant__ WinArgs a) {
     }
     __syncthreads();
     for (int r = tid / 32; key0 + r < end && r < kTile; r += kThreads / 32)
-        if (s_bad[r]) {
+        if (s_bad[r] && key_tainted<T>(a, it.b, it.h, key0 + r, len, it.stop)) {
             const int c = 2 * (tid % 32);
             const bool sum = it.part == 0 && r < a.sinks;
             const KeyRow k = redo_dkv_row<T>(a, it.b, it.h, key0 + r, len, sum ? row_end : len);
@@ -502,6 +514,13 @@ void plan_parts(WinArgs& a, int tile) {
     a.parts = (int)((a.n - split + a.part_rows - 1) / a.part_rows);
 }
 static bool on_tensor_cores(const psk_window_shape* sh) { return sh->dtype == PSK_BF16 && sh->path != PSK_PATH_CUDA_CORES; }
+// Device waits are bounded by a second, and some last as long as a tile: 2^25 rows of query heads on one tile of keys take the key side 0.4 s.
+static int check_attention(const psk_window_shape* sh) {
+    const int st = check_rows(sh);
+    if (st != PSK_OK || !on_tensor_cores(sh)) return st;
+    const int64_t band = (int64_t)sh->window + 128, rows = sh->sinks > 0 || band > sh->n ? sh->n : band;
+    return rows * (sh->H / sh->Hkv) < (int64_t)1 << 25 ? PSK_OK : PSK_ERR_UNSUPPORTED;
+}
 WinArgs args_of(const psk_window_shape* sh) {
     WinArgs a{};
     a.B = sh->B; a.H = sh->H; a.Hkv = sh->Hkv; a.G = sh->H / sh->Hkv; a.n = sh->n;
@@ -522,7 +541,7 @@ using namespace psk::win;
 extern "C" {
 
 size_t psk_window_workspace_bytes(const psk_window_shape* shape, int for_backward) {
-    if (check_rows(shape) != PSK_OK) return 0;
+    if (check_attention(shape) != PSK_OK) return 0;
     if (!for_backward) return kStatusBytes;
     WinArgs a = args_of(shape);
     size_t parts = 0;                                     // (enough for either path)
@@ -536,7 +555,7 @@ size_t psk_window_workspace_bytes(const psk_window_shape* shape, int for_backwar
 
 int psk_window_attn_fwd(const psk_window_shape* shape, const void* Q, const void* K, const void* V, const int32_t* lengths, void* O, float* lse,
                         void* workspace, size_t workspace_bytes, void* stream) {
-    const int st = check_rows(shape);
+    const int st = check_attention(shape);
     if (st != PSK_OK) return st;
     if (!Q || !K || !V || !O || !lse) return PSK_ERR_INVALID_ARG;
     for (const void* p : {Q, K, V, (const void*)O})
@@ -559,7 +578,7 @@ int psk_window_attn_fwd(const psk_window_shape* shape, const void* Q, const void
 
 int psk_window_attn_bwd(const psk_window_shape* shape, const void* Q, const void* K, const void* V, const int32_t* lengths, const void* O,
                         const float* lse, const void* dO, void* dQ, void* dK, void* dV, void* workspace, size_t workspace_bytes, void* stream) {
-    const int st = check_rows(shape);
+    const int st = check_attention(shape);
     if (st != PSK_OK) return st;
     if (!Q || !K || !V || !O || !lse || !dO || !dQ || !dK || !dV) return PSK_ERR_INVALID_ARG;
     for (const void* p : {Q, K, V, O, dO, (const void*)dQ, (const void*)dK, (const void*)dV})

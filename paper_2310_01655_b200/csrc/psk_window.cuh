@@ -52,45 +52,82 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 __device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000); }
 __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
 
-__device__ __forceinline__ float warp_sum(float v) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
-}
-
 // ---- single rows by one warp, pair by pair ----
 // The tiled kernels multiply the weight 0 of a pair that the mask leaves out with the other row's values.  If an infinity or a NaN
-// stands there, it comes through as NaN.  So a result row that is not finite is formed again here from
-// the pairs that count alone (lane l holds columns 2 l and 2 l + 1).  Slow, and only there.
+// stands there, it comes through as NaN.  So a result row that is not finite, though its own statistics are no NaN, and that shares a tile with
+// such a row that it does not see (*_tainted) is formed again here from the pairs that count alone (lane l holds columns 2 l and
+// 2 l + 1).  Slow, and only there: eight pairs on their way at a time, and no further than to the pair that makes all of
+// the row NaN.  (The other warps wait for this one, with a limit of a second.)
+constexpr int kRedo = 8;
 template <typename T> __device__ __forceinline__ float2 ld2(const T* p) { return make_float2(ldf(p), ldf(p + 1)); }
 template <typename T> __device__ __forceinline__ void st2(T* p, float2 v) { stf(p, v.x); stf(p + 1, v.y); }
-__device__ __forceinline__ float dot2(float2 a, float2 b) { return warp_sum(fmaf(a.x, b.x, a.y * b.y)); }
+__device__ __forceinline__ float dot2(float2 a, float2 b) { return fmaf(a.x, b.x, a.y * b.y); }
+__device__ __forceinline__ bool all_nan(float2 v) { return __all_sync(0xffffffffu, v.x != v.x && v.y != v.y); }
+__device__ __forceinline__ void warp_sums(float (&v)[kRedo]) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+        for (int u = 0; u < kRedo; ++u) v[u] += __shfl_xor_sync(0xffffffffu, v[u], o);
+}
+// The keys of row i by number: those of the sinks before its window, then its window.
+struct RowKeys {
+    int lo, first;
+    __device__ __forceinline__ RowKeys(int i, int window, int sinks) : lo(window_start(i, window)) { first = sinks < lo ? sinks : lo; }
+    __device__ __forceinline__ int count(int i) const { return first + i - lo + 1; }
+    __device__ __forceinline__ int at(int t) const { return t < first ? t : lo + t - first; }
+};
 
-template <typename F>
-__device__ __forceinline__ void for_keys(int i, int window, int sinks, F&& f) {
-    const int lo = window_start(i, window), first = sinks < lo ? sinks : lo;
-    for (int j = 0; j < first; ++j) f(j);
-    for (int j = lo; j <= i; ++j) f(j);
+// Is any value of the rows r0 .. r1 - 1 of A or B not finite?
+template <typename T>
+__device__ __noinline__ bool rows_tainted(const T* A, const T* B, int64_t stride, int r0, int r1) {
+    const int l2 = 2 * (threadIdx.x % 32);
+    float zero = 0.f;                                     // (becomes NaN with any infinity or NaN)
+#pragma unroll 8
+    for (int r = r0; r < r1; ++r) {
+        const float2 a = ld2(A + r * stride + l2), b = ld2(B + r * stride + l2);
+        zero += a.x * 0.f + a.y * 0.f + b.x * 0.f + b.y * 0.f;
+    }
+    return __any_sync(0xffffffffu, zero != 0.f);
+}
+// Query side, row i of a sequence of `len`: keys that it does not see and that tiles of up to 128 rows and keys bring with it.
+template <typename T>
+__device__ __noinline__ bool row_tainted(const T* K, const T* V, int64_t kn, int i, int window, int sinks, int len) {
+    const int lo = window_start(i, window), before = lo > 256 ? lo - 256 : 0, after = len - i > 128 ? i + 128 : len;
+    const int64_t tile = ((int64_t)sinks + 127) / 128 * 128;
+    return rows_tainted(K, V, kn, before, lo) || rows_tainted(K, V, kn, i + 1, after) || (sinks > 0 && rows_tainted(K, V, kn, sinks, (int)(tile < lo ? tile : lo)));
 }
 
-// q, K, V: of row i and of its head; lse: its place, or null
+// q, K, V: of row i and of its head
 template <typename T>
-__device__ __noinline__ float2 redo_out_row(const T* q, const T* K, const T* V, int64_t kn, int i, int window, int sinks, float c, float* lse) {
+__device__ __noinline__ float2 redo_out_row(const T* q, const T* K, const T* V, int64_t kn, int i, int window, int sinks, float c) {
     const int l2 = 2 * (threadIdx.x % 32);
     const float2 qv = ld2(q + l2);
+    const RowKeys keys(i, window, sinks);
+    const int count = keys.count(i);
     float m = neg_inf(), l = 0.f;
     float2 acc = make_float2(0.f, 0.f);
-    for_keys(i, window, sinks, [&](int j) {
-        const float s = dot2(qv, ld2(K + j * kn + l2)) * c;
-        const float m2 = fmaxf(m, s);                     // (a NaN score: p is NaN, and so is the row)
-        const float base = m2 == neg_inf() ? 0.f : m2, alpha = exp2_approx(m - base), p = exp2_approx(s - base);
-        const float2 v = ld2(V + j * kn + l2);
-        acc.x = fmaf(acc.x, alpha, p * v.x);
-        acc.y = fmaf(acc.y, alpha, p * v.y);
-        l = fmaf(l, alpha, p);
-        m = m2;
-    });
-    if (l2 == 0 && lse != nullptr) *lse = (m + log2f(l)) * kLn2;
+#pragma unroll 1
+    for (int t = 0; t < count && !all_nan(acc); t += kRedo) {
+        float s[kRedo];
+        float2 v[kRedo];
+#pragma unroll
+        for (int u = 0; u < kRedo; ++u) {
+            const int64_t at = keys.at(t + u < count ? t + u : t) * kn + l2;
+            s[u] = dot2(qv, ld2(K + at));
+            v[u] = ld2(V + at);
+        }
+        warp_sums(s);
+#pragma unroll
+        for (int u = 0; u < kRedo; ++u) {
+            if (t + u >= count) break;
+            const float x = s[u] * c, m2 = fmaxf(m, x);   // (a NaN score: p is NaN, and so is the row)
+            const float base = m2 == neg_inf() ? 0.f : m2, alpha = exp2_approx(m - base), p = exp2_approx(x - base);
+            acc.x = fmaf(acc.x, alpha, p * v[u].x);
+            acc.y = fmaf(acc.y, alpha, p * v[u].y);
+            l = fmaf(l, alpha, p);
+            m = m2;
+        }
+    }
     return make_float2(acc.x / l, acc.y / l);
 }
 
@@ -99,15 +136,55 @@ __device__ __noinline__ float2 redo_dq_row(const T* q, const T* dO, const T* K, 
                                            float2 stat) {
     const int l2 = 2 * (threadIdx.x % 32);
     const float2 qv = ld2(q + l2), dv = ld2(dO + l2);
+    const RowKeys keys(i, window, sinks);
+    const int count = keys.count(i);
     float2 acc = make_float2(0.f, 0.f);
-    for_keys(i, window, sinks, [&](int j) {
-        const float2 k = ld2(K + j * kn + l2);
-        const float p = exp2_approx(fmaf(dot2(qv, k), c, -stat.x));
-        const float ds = p * (dot2(dv, ld2(V + j * kn + l2)) - stat.y);
-        acc.x = fmaf(ds, k.x, acc.x);
-        acc.y = fmaf(ds, k.y, acc.y);
-    });
+#pragma unroll 1
+    for (int t = 0; t < count && !all_nan(acc); t += kRedo) {
+        float s[kRedo], d[kRedo];
+        float2 k[kRedo];
+#pragma unroll
+        for (int u = 0; u < kRedo; ++u) {
+            const int64_t at = keys.at(t + u < count ? t + u : t) * kn + l2;
+            k[u] = ld2(K + at);
+            s[u] = dot2(qv, k[u]);
+            d[u] = dot2(dv, ld2(V + at));
+        }
+        warp_sums(s);
+        warp_sums(d);
+#pragma unroll
+        for (int u = 0; u < kRedo; ++u) {
+            if (t + u >= count) break;
+            const float ds = exp2_approx(fmaf(s[u], c, -stat.x)) * (d[u] - stat.y);
+            acc.x = fmaf(ds, k[u].x, acc.x);
+            acc.y = fmaf(ds, k[u].y, acc.y);
+        }
+    }
     return make_float2(acc.x * scale, acc.y * scale);
+}
+
+// Key side, key j: query rows that do not see it and that tiles bring with it (keys in tiles of up to 128, rows in steps of up to 64, before `stop`).
+template <typename T>
+__device__ __noinline__ bool key_tainted(const WinArgs& a, int b, int hk, int j, int len, int stop) {
+    const int64_t past = (int64_t)j + a.window;
+    const int before = j > 127 ? j - 127 : 0, most = len < stop ? len : stop;
+    int r0 = most, r1 = most;                             // behind its window
+    if (j >= a.sinks && past < most) {
+        r0 = (int)past;
+        if (j / 128 * 128 >= a.sinks && most - r0 > 192) r1 = r0 + 192;
+        if (r1 - r0 > a.window + 192) return true;        // (more rows than those that count: look at these instead)
+    }
+    for (int g = 0; g < a.G; ++g) {
+        const int h = hk * a.G + g;
+        const int64_t at = b * a.qb + h * a.qh;
+        if (rows_tainted((const T*)a.Q + at, (const T*)a.dO + at, a.qn, before, j) || rows_tainted((const T*)a.Q + at, (const T*)a.dO + at, a.qn, r0, r1)) return true;
+        const float *sl = a.stat_l + ((int64_t)b * a.H + h) * a.n, *sd = a.stat_d + ((int64_t)b * a.H + h) * a.n;
+        bool bad = false;
+        for (int r = before + (int)(threadIdx.x % 32); r < j; r += 32) bad = bad || !finite(sl[r]) || !finite(sd[r]);
+        for (int r = r0 + (int)(threadIdx.x % 32); r < r1; r += 32) bad = bad || !finite(sl[r]) || !finite(sd[r]);
+        if (__any_sync(0xffffffffu, bad)) return true;
+    }
+    return false;
 }
 
 // row j of key head hk of sequence b: (dk, dv), from the query rows before `stop`
@@ -122,14 +199,29 @@ __device__ __noinline__ KeyRow redo_dkv_row(const WinArgs& a, int b, int hk, int
     const int most = len < stop ? len : stop, end = (j < a.sinks || past > most) ? most : (int)past;
     for (int g = 0; g < a.G; ++g) {
         const int h = hk * a.G + g;
-        for (int i = j; i < end; ++i) {
-            const int64_t row = b * a.qb + h * a.qh + i * a.qn + l2;
-            const int64_t at = ((int64_t)b * a.H + h) * a.n + i;
-            const float2 q = ld2((const T*)a.Q + row), d = ld2((const T*)a.dO + row);
-            const float p = exp2_approx(fmaf(dot2(q, k), a.c, a.stat_l[at]));
-            const float ds = p * (dot2(d, v) + a.stat_d[at]) * a.scale;
-            r.dv.x = fmaf(p, d.x, r.dv.x); r.dv.y = fmaf(p, d.y, r.dv.y);
-            r.dk.x = fmaf(ds, q.x, r.dk.x); r.dk.y = fmaf(ds, q.y, r.dk.y);
+        const T *Q = (const T*)a.Q + b * a.qb + h * a.qh + l2, *dO = (const T*)a.dO + b * a.qb + h * a.qh + l2;
+        const float *sl = a.stat_l + ((int64_t)b * a.H + h) * a.n, *sd = a.stat_d + ((int64_t)b * a.H + h) * a.n;
+#pragma unroll 1
+        for (int i0 = j; i0 < end && !(all_nan(r.dk) && all_nan(r.dv)); i0 += kRedo) {
+            float s[kRedo], e[kRedo];
+            float2 q[kRedo], d[kRedo];
+#pragma unroll
+            for (int u = 0; u < kRedo; ++u) {
+                const int i = end - i0 > u ? i0 + u : i0;
+                q[u] = ld2(Q + i * a.qn);
+                d[u] = ld2(dO + i * a.qn);
+                s[u] = dot2(q[u], k);
+                e[u] = dot2(d[u], v);
+            }
+            warp_sums(s);
+            warp_sums(e);
+#pragma unroll
+            for (int u = 0; u < kRedo; ++u) {
+                if (end - i0 <= u) break;
+                const float p = exp2_approx(fmaf(s[u], a.c, sl[i0 + u])), ds = p * (e[u] + sd[i0 + u]) * a.scale;
+                r.dv.x = fmaf(p, d[u].x, r.dv.x); r.dv.y = fmaf(p, d[u].y, r.dv.y);
+                r.dk.x = fmaf(ds, q[u].x, r.dk.x); r.dk.y = fmaf(ds, q[u].y, r.dk.y);
+            }
         }
     }
     return r;

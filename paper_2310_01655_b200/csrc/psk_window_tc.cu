@@ -426,17 +426,16 @@ tc_win_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
                 const float v = (m * c + log2f(l)) * kLn2;
                 ok = mbar_wait(&bar_o, (t - 1) & 1, status, kErrMma) && ok;
                 tc_fence_after();
-                const bool fine = stage_half(st, row, half, lane_tm + Fwd::cO, 1.f / l, live) && finite(v);
+                const bool fine = stage_half(st, row, half, lane_tm + Fwd::cO, 1.f / l, live) || !finite(v);      // (where v is not, the row is NaN)
                 tc_fence_before();
                 if (ok && half == 0 && i < a.n) lse[i] = live ? v : neg_inf();
-                const unsigned lost = __ballot_sync(0xffffffffu, !finite(v));
                 unsigned bad = __ballot_sync(0xffffffffu, ok && !fine && live);
                 while (bad != 0) {
                     const int k = __ffs(bad) - 1, r = i_first + k, hk = p.h / a.G;
                     bad &= bad - 1;
-                    const int64_t koff = p.b * a.kb + hk * a.kh;
-                    stage_pair(st, warp % 4 * 32 + k, redo_out_row((const bf16*)a.Q + p.b * a.qb + p.h * a.qh + (int64_t)r * a.qn, (const bf16*)a.K + koff,
-                               (const bf16*)a.V + koff, a.kn, r, a.window, a.sinks, c, half == 0 && (lost >> k & 1u) ? lse + r : nullptr), half);
+                    const bf16 *K = (const bf16*)a.K + p.b * a.kb + hk * a.kh, *V = (const bf16*)a.V + p.b * a.kb + hk * a.kh;
+                    if (row_tainted(K, V, a.kn, r, a.window, a.sinks, p.len))
+                        stage_pair(st, warp % 4 * 32 + k, redo_out_row((const bf16*)a.Q + p.b * a.qb + p.h * a.qh + (int64_t)r * a.qn, K, V, a.kn, r, a.window, a.sinks, c), half);
                 }
                 fence_proxy_async_smem();
                 bar_sync(5, Fwd::kRowThreads);
@@ -700,15 +699,16 @@ tc_win_dq_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
                     bar_sync(1 + group, kRows);
                     const bool live = i < p.len, fine = stage_row(st, row, lane_tm + Dq::cDq, a.scale, live);
                     tc_fence_before();
-                    unsigned bad = __ballot_sync(0xffffffffu, ok && !fine && live);
+                    unsigned bad = __ballot_sync(0xffffffffu, ok && !fine && live && stat.x == stat.x && stat.y == stat.y);      // (with a NaN there the row is NaN)
                     if (lane == 0) mbar_arrive(&bar_acc);
                     while (bad != 0) {
                         const int k = __ffs(bad) - 1, r = i_first + k, hk = p.h / a.G;
                         bad &= bad - 1;
-                        const int64_t at = qoff + (int64_t)r * a.qn, koff = p.b * a.kb + hk * a.kh;
+                        const int64_t at = qoff + (int64_t)r * a.qn;
+                        const bf16 *K = (const bf16*)a.K + p.b * a.kb + hk * a.kh, *V = (const bf16*)a.V + p.b * a.kb + hk * a.kh;
                         const float2 sr = make_float2(-__shfl_sync(0xffffffffu, stat.x, k), -__shfl_sync(0xffffffffu, stat.y, k));
-                        stage_pair(st, warp % 4 * 32 + k, redo_dq_row((const bf16*)a.Q + at, (const bf16*)a.dO + at, (const bf16*)a.K + koff, (const bf16*)a.V + koff,
-                                                                      a.kn, r, a.window, a.sinks, a.c, a.scale, sr));
+                        if (row_tainted(K, V, a.kn, r, a.window, a.sinks, p.len))
+                            stage_pair(st, warp % 4 * 32 + k, redo_dq_row((const bf16*)a.Q + at, (const bf16*)a.dO + at, K, V, a.kn, r, a.window, a.sinks, a.c, a.scale, sr));
                     }
                     fence_proxy_async_smem();
                     bar_sync(1 + group, kRows);
@@ -967,6 +967,7 @@ tc_win_dkv_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constan
                             const int k = __ffs(bad) - 1, r = warp % 4 * 32 + k;
                             bad &= bad - 1;
                             const bool part = PARTS && p.part == 0 && r < a.sinks;
+                            if (!key_tainted<bf16>(a, p.b, p.h, j_first + k, p.len, p.stop)) continue;
                             const KeyRow key = redo_dkv_row<bf16>(a, p.b, p.h, j_first + k, p.len, part ? p.stop : p.len);
                             stage_pair(st, r, has_k ? key.dk : key.dv);
                             if (part) st2(partial_row(a, p.b, p.h, 0, has_k ? 0 : 1, r) + 2 * lane, has_k ? key.dk : key.dv);

@@ -197,6 +197,45 @@ def test_masked_infinities_and_nans(dtype, path, bad, window, sinks):
 
 
 @pytest.mark.parametrize("dtype,path", PATHS)
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+@pytest.mark.parametrize("which", ["q row", "k row", "k", "v", "dO", "all"])
+@pytest.mark.parametrize("window,sinks", [(70, 0), (60, 130), (2000, 0)])
+def test_infinities_and_nans_that_are_seen(dtype, path, bad, which, window, sinks):
+    """What is not finite by the formulas, and only that, comes out so; all else is as if alone."""
+    n, s = 420, 131
+    Q, K, V, dO = make(dtype, 1, 2, 1, n, seed=29)
+    if which == "q row":
+        Q[0, 1, s] = bad
+    elif which == "k row":
+        K[0, 0, s] = bad
+    elif which == "k":
+        K[0, 0, s, 9] = bad
+    elif which == "v":
+        V[0, 0, s, 9] = bad
+    elif which == "dO":
+        dO[0, 1, s, 9] = bad
+    else:
+        for x in (Q, K, V, dO):
+            x.fill_(bad)
+    got = run(Q, K, V, dO, window, sinks, path=path)
+    with np.errstate(all="ignore"):
+        dk = dv = 0.0
+        pairs = []
+        for h in range(2):
+            a = (f64(Q[0, h]), f64(K[0, 0]), f64(V[0, 0]))
+            O, lse, _ = orc.window_attention(*a, window, sinks, 0.125)
+            rq, rk, rv = orc.window_attention_backward(*a, f64(dO[0, h]), window, sinks, 0.125)
+            pairs += [("O", got[0][0, h], O), ("lse", got[1][0, h], lse), ("dQ", got[2][0, h], rq)]
+            dk, dv = dk + rk, dv + rv
+        pairs += [("dK", got[3][0, 0], dk), ("dV", got[4][0, 0], dv)]
+        for name, x, y in pairs:
+            x = f64(x)
+            fine = np.isfinite(y)
+            assert np.array_equal(np.isfinite(x), fine), name
+            assert np.linalg.norm((x - y)[fine]) <= 4 * max(E[dtype], 1e-6) * np.linalg.norm(y[fine]), name
+
+
+@pytest.mark.parametrize("dtype,path", PATHS)
 def test_large_scores(dtype, path):
     # weights that are one or nothing, scores in the hundreds, growing along the row so that the running maximum moves on
     n, window = 300, 170

@@ -82,6 +82,17 @@ def test_window_rows(L, fields, code):
     assert L.psk_window_workspace_bytes(byref(s), 1) == 0
 
 
+@pytest.mark.parametrize("window,sinks,path,ok", [(32, 0, 0, True), (1 << 22, 0, 0, False), (2**31 - 1, 0, 2, False), (32, 1, 0, False), ((1 << 21) - 129, 0, 0, True),
+                                                  ((1 << 21) - 128, 0, 0, False), (1 << 22, 3, 1, True)])
+def test_window_longest_tiles(L, window, sinks, path, ok):
+    """A tile of keys on the tensor cores is worked on for less than the second that a wait lasts at most."""
+    n = 1 << 22
+    s = WindowShape(1, 16, 1, n, 64, window, sinks, 1, path, 0.125, 64 * n * 16, 64 * n, 64, 64 * n, 64 * n, 64)
+    assert [L.psk_window_workspace_bytes(byref(s), k) > 0 for k in (0, 1)] == [ok, ok]
+    if not ok:
+        assert window_calls(L, s)[:2] == (-2, -2)
+
+
 def test_window_cache_too_large(L):
     s = window()
     s.window, s.sinks = 2**31 - 1, 5
