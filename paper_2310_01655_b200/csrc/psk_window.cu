@@ -13,14 +13,15 @@ namespace {
 using namespace cc;
 
 // ---------------------------------------------------------------------------
-// Forward and backward by 64 x 64 tiles, 64 threads (two warps) to a CTA, 8 x 8 of every product to a thread (cc_gemm.cuh).
-// Bound: fp32 FMA rate and the shared-memory loads behind it.  One tile of rows to a CTA, so that three to four CTAs share an
-// SM and one's loads hide behind another's products; a tile whose values are used up gives its place to the weights.
+// Forward and backward by tiles of 64 rows (or keys), 128 threads to a CTA, three CTAs to an SM; the forward in steps of 64 keys, the backward in
+// steps of 32.  Bound: fp32 FMA rate, and the latency of what stands between the products: more, smaller threads win (24 heads x 2048
+// rows, window 256, one sink, forward / query side / key side: 143 / 201 / 252 us; 64 threads with 8 x 8 values each, at most 255 registers
+// and so 6 to 8 warps to an SM, 198 / 247 / 388).
 // ---------------------------------------------------------------------------
-constexpr int kTile = 64, kThreads = 64;
+constexpr int kTile = 64, kThreads = 128;
 
-// ROWS rows x 64 columns from row r0 into [ROWS][kLd] fp32, zeros from row `end` on.  fp32: asynchronous copies, all on their way at once (forward
-// of 24 heads x 2048 rows, window 256: 198 us; through registers, in batches of four, 215 with 190 at the time); cp_wait<> before the barrier in front of their use.
+// ROWS rows x 64 columns from row r0 into [ROWS][kLd] fp32, zeros from row `end` on.  fp32: asynchronous copies, all on their way at once (through
+// registers, in batches of four: the forward 13 % slower); cp_wait<> before the barrier in front of their use.
 template <int ROWS = kTile, typename T>
 __device__ __forceinline__ void load_tile(float* dst, const T* src, int64_t stride, int r0, int end) {
     constexpr int V = 16 / sizeof(T), PerRow = 64 / V;
@@ -56,19 +57,71 @@ __device__ __forceinline__ void store4(T* p, float a, float b, float c, float d)
         *reinterpret_cast<uint2*>(p) = make_uint2(u, v);
     }
 }
-// Accumulator row i times f, as the thread's 8 of 64 columns; false if one of the row's 64 is not finite (the same in its 8 lanes).
-__device__ __forceinline__ bool row_out(const Acc& acc, int i, float f, float (&o)[8]) {
-    bool fine = true;
+// Half of a 64 x 64 accumulator in the outer form: the thread's 8 rows and 4 columns of one half (32 columns) each.
+struct HalfAcc {
+    f2 s[4][2], x[4][2];              // straight / swapped column pairs
+    __device__ __forceinline__ void zero() {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) { o[j] = acc.at(i, j) * f; fine = fine && finite(o[j]); }
-    const unsigned all = __ballot_sync(0xffffffffu, fine);
-    return (all >> (threadIdx.x % 32 / 8 * 8) & 0xffu) == 0xffu;
+        for (int p = 0; p < 4; ++p)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) s[p][q] = x[p][q] = 0ull;
+    }
+    // += At^T B over k < K: At [K][kLd] (64 rows), B [K][kLd], from the thread's columns on
+    __device__ __forceinline__ void add(const float* At, const float* B, int K, int ry) {
+#pragma unroll 4
+        for (int k = 0; k < K; ++k) {
+            f2 a[4];
+            load_rows8(a, At + k * kLd + 8 * ry);
+            const F22 b = lds22(B + k * kLd);
+            const f2 c[2] = {b.x, b.y};
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const f2 sw = swap2(c[q]);
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    s[p][q] = fma2(a[p], c[q], s[p][q]);
+                    x[p][q] = fma2(a[p], sw, x[p][q]);
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ float at(int i, int j) const {
+        const f2 v = ((i ^ j) & 1) ? x[i / 2][j / 2] : s[i / 2][j / 2];
+        return (i & 1) ? hi2(v) : lo2(v);
+    }
+    // Row i times f; false if one of the half's 32 values is not finite (the same in its 8 lanes).
+    __device__ __forceinline__ bool row(int i, float f, float (&o)[4]) const {
+        bool fine = true;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { o[j] = at(i, j) * f; fine = fine && finite(o[j]); }
+        const unsigned all = __ballot_sync(0xffffffffu, fine);
+        return (all >> (threadIdx.x % 32 / 8 * 8) & 0xffu) == 0xffu;
+    }
+};
+// d[i][j] = sum_{k < 64} A[ry + 8 i][k] B[cx + 8 j][k], four rows by four columns.
+__device__ __forceinline__ void dot_quarter(f2 (&d)[4][4], const float* A, const float* B, int ry, int cx) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) d[i][j] = 0ull;
+    const float *a0 = A + ry * kLd, *b0 = B + cx * kLd;
+#pragma unroll 4
+    for (int k = 0; k < 64; k += 4) {
+        F22 a[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = lds22(a0 + 8 * i * kLd + k);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const F22 b = lds22(b0 + 8 * j * kLd + k);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                d[i][j] = fma2(a[i].x, b.x, d[i][j]);
+                d[i][j] = fma2(a[i].y, b.y, d[i][j]);
+            }
+        }
+    }
 }
-template <typename T>
-__device__ __forceinline__ void store_row(T* p, int cx, const float (&o)[8]) {
-    store4(p + 4 * cx, o[0], o[1], o[2], o[3]);
-    store4(p + 32 + 4 * cx, o[4], o[5], o[6], o[7]);
-}
+template <typename T> __device__ __forceinline__ void store_row(T* p, const float (&o)[4]) { store4(p, o[0], o[1], o[2], o[3]); }
 template <typename T>
 __device__ __forceinline__ void zero_rows(T* p, int64_t stride, int r0, int end) {
     for (int e = threadIdx.x; e < kTile * 16; e += kThreads)
@@ -107,15 +160,15 @@ __device__ __noinline__ void redo_out_rows(const WinArgs& a, const int* bad) {
 constexpr size_t kFwdSmem = 4 * kUnit * sizeof(float);
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 3)
 win_fwd_kernel(const __grid_constant__ WinArgs a) {
     pdl_sync();
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0;
     extern __shared__ float sm[];
     __shared__ float s_al[kTile], s_inv[kTile];
-    __shared__ int s_bad[kTile];
+    __shared__ int s_nan[kTile], s_bad[kTile];
     float *sQ = sm, *sK = sm + kUnit, *sV = sm + 2 * kUnit, *sP = sm + 3 * kUnit;
-    const int tid = threadIdx.x, ry = tid / 8, cx = tid % 8;
+    const int tid = threadIdx.x, half = tid / 64, ry = tid % 64 / 8, cx = tid % 8, col = 32 * half + 4 * cx;
     const Place pl = place_of(a, a.H);
     const T* Q = (const T*)a.Q + pl.b * a.qb + pl.h * a.qh;
     const int64_t koff = pl.b * a.kb + pl.h / a.G * a.kh;
@@ -128,10 +181,11 @@ win_fwd_kernel(const __grid_constant__ WinArgs a) {
     for (int r = (end > row0 ? end : row0) + tid; r < n_end; r += kThreads) lse[r] = neg_inf();
     if (end <= row0) return;
     load_tile(sQ, Q, a.qn, row0, end);
-    float m[8], l[8];
+    // scores: rows ry + 32 half + 8 i, columns cx + 8 j
+    float m[4], l[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { m[i] = neg_inf(); l[i] = 0.f; }
-    Acc acc;
+    for (int i = 0; i < 4; ++i) { m[i] = neg_inf(); l[i] = 0.f; }
+    HalfAcc acc;
     acc.zero();
     const KeyTiles kt = key_tiles(row0, end - 1, a.window, a.sinks, kTile);
     const int steps = kt.count();
@@ -142,20 +196,18 @@ win_fwd_kernel(const __grid_constant__ WinArgs a) {
         cp_wait<1>();                                     // the keys; the values may still be on their way
         __syncthreads();
         const bool whole = sees_all(row0, kTile, k0, kTile, a.window, a.sinks);
-        float p[8][8];
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
+        {
             f2 d[4][8];
             dot_half<kLd, kLd>(d, sQ, sK, 16, half, ry, cx);
 #pragma unroll
-            for (int i4 = 0; i4 < 4; ++i4) {
-                const int i = 4 * half + i4, row = row0 + ry + 8 * i;
-                float top = m[i];
+            for (int i = 0; i < 4; ++i) {
+                const int r = ry + 32 * half + 8 * i;
+                float p[8], top = m[i];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float s = sum2(d[i4][j]) * a.c;
-                    p[i][j] = whole || sees(row, k0 + cx + 8 * j, a.window, a.sinks) ? s : neg_inf();
-                    top = fmaxf(top, p[i][j]);
+                    const float s = sum2(d[i][j]) * a.c;
+                    p[j] = whole || sees(row0 + r, k0 + cx + 8 * j, a.window, a.sinks) ? s : neg_inf();
+                    top = fmaxf(top, p[j]);
                 }
 #pragma unroll
                 for (int o = 1; o < 8; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
@@ -163,14 +215,14 @@ win_fwd_kernel(const __grid_constant__ WinArgs a) {
                 m[i] = top;
                 l[i] *= alpha;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) { p[i][j] = exp2_approx(p[i][j] - base); l[i] += p[i][j]; }
-                if (cx == 0) s_al[ry + 8 * i] = alpha;
+                for (int j = 0; j < 8; ++j) {
+                    p[j] = exp2_approx(p[j] - base);
+                    l[i] += p[j];
+                    sP[(cx + 8 * j) * kLd + r] = p[j];
+                }
+                if (cx == 0) s_al[r] = alpha;
             }
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sP[(cx + 8 * j) * kLd + ry + 8 * i] = p[i][j];
         cp_wait<0>();                                     // the values
         __syncthreads();                                  // everyone has read the keys
         if (x + 1 < steps) load_tile(sK, K, a.kn, kt.at(x + 1) * kTile, len);
@@ -178,21 +230,22 @@ win_fwd_kernel(const __grid_constant__ WinArgs a) {
         for (int p2 = 0; p2 < 4; ++p2) {
             const f2 al = *reinterpret_cast<const f2*>(s_al + 8 * ry + 2 * p2);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) { acc.s[p2][q] = mul2(acc.s[p2][q], al); acc.x[p2][q] = mul2(acc.x[p2][q], al); }
+            for (int q = 0; q < 2; ++q) { acc.s[p2][q] = mul2(acc.s[p2][q], al); acc.x[p2][q] = mul2(acc.x[p2][q], al); }
         }
-        outer_product(acc, sP, sV, kTile, kLd, ry, cx);
+        acc.add(sP, sV + col, kTile, ry);
         __syncthreads();
         if (x + 1 < steps) load_tile(sV, V, a.kn, kt.at(x + 1) * kTile, len);
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 4; ++i) {
 #pragma unroll
         for (int o = 1; o < 8; o <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], o);
         if (cx == 0) {
-            const int r = ry + 8 * i;
+            const int r = ry + 32 * half + 8 * i;
             const float v = (m[i] + log2f(l[i])) * kLn2;
             s_inv[r] = 1.f / l[i];
-            s_bad[r] = !finite(v);
+            s_nan[r] = !finite(v);                        // (then neither is the row: NaN)
+            s_bad[r] = 0;
             if (row0 + r < end) lse[row0 + r] = v;
         }
     }
@@ -200,33 +253,31 @@ win_fwd_kernel(const __grid_constant__ WinArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int r = out_row(ry, i);
-        float o[8];
-        // (where the statistics are not finite, neither is the row: NaN)
-        const bool fine = row_out(acc, i, s_inv[r], o) || s_bad[r];
-        __syncwarp();
-        if (row0 + r < end) store_row(O + (int64_t)(row0 + r) * a.qn, cx, o);
-        if (cx == 0) s_bad[r] = !fine;
+        float o[4];
+        const bool fine = acc.row(i, s_inv[r], o);
+        if (row0 + r < end) store_row(O + (int64_t)(row0 + r) * a.qn + col, o);
+        if (!fine && !s_nan[r]) s_bad[r] = 1;
     }
     __syncthreads();
     redo_out_rows<T>(a, s_bad);
 }
 
-// Keys (query side) or query rows (key side) of a step of the backward: with 32 four CTAs (three) fit into an SM, with 64 three (two):
-// 24 heads x 2048 rows, window 256: 247 + 412 us against 278 + 442.
+// Keys (query side) or query rows (key side) of a step of the backward.  32: less of a window's edges is computed for nothing, and three CTAs fit
+// on the key side (us with 32 / 64: window 256 as above 201 / 218 and 252 / 266; causal, 4 heads x 4096: 779 / 787 and 921 / 893).
 constexpr int kStep = 32;
-constexpr size_t kDqSmem = 3 * kUnit * sizeof(float);
+constexpr size_t kDqSmem = 4 * kUnit * sizeof(float);
 
 // The gradient of 64 query rows; their statistics on the way, which the key side reads.
 template <typename T>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 3)
 win_dq_kernel(const __grid_constant__ WinArgs a) {
     pdl_sync();
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0;
     extern __shared__ float sm[];
     __shared__ float s_D[kTile], s_lse[kTile];
     __shared__ int s_bad[kTile];
-    float *sQ = sm, *sG = sm + kUnit, *sK = sm + 2 * kUnit, *sV = sK + kStep * kLd, *sP = sV;      // ds takes the values' place
-    const int tid = threadIdx.x, ry = tid / 8, cx = tid % 8;
+    float *sQ = sm, *sG = sm + kUnit, *sK = sm + 2 * kUnit, *sV = sK + 2 * kStep * kLd, *sP = sV + kStep * kLd;
+    const int tid = threadIdx.x, half = tid / 64, ry = tid % 64 / 8, cx = tid % 8, col = 32 * half + 4 * cx;
     const Place pl = place_of(a, a.H);
     const int64_t qoff = pl.b * a.qb + pl.h * a.qh, koff = pl.b * a.kb + pl.h / a.G * a.kh, soff = ((int64_t)pl.b * a.H + pl.h) * a.n;
     const T *Q = (const T*)a.Q + qoff, *dO = (const T*)a.dO + qoff, *O = (const T*)a.O + qoff, *K = (const T*)a.K + koff, *V = (const T*)a.V + koff;
@@ -240,7 +291,7 @@ win_dq_kernel(const __grid_constant__ WinArgs a) {
     load_tile(sK, O, a.qn, row0, end);
     cp_wait<0>();
     __syncthreads();
-    {
+    if (tid < kTile) {
         float D = 0.f;
 #pragma unroll 8
         for (int c = 0; c < 64; ++c) D = fmaf(sG[tid * kLd + c], sK[tid * kLd + c], D);
@@ -248,53 +299,58 @@ win_dq_kernel(const __grid_constant__ WinArgs a) {
         s_lse[tid] = row0 + tid < end ? a.lse_in[soff + row0 + tid] * kLog2e : 0.f;
         if (row0 + tid < end) { a.stat_l[soff + row0 + tid] = -s_lse[tid]; a.stat_d[soff + row0 + tid] = -D; }
     }
-    Acc acc;
+    HalfAcc acc;
     acc.zero();
     const KeyTiles kt = key_tiles(row0, end - 1, a.window, a.sinks, kStep);
-    for (int x = 0; x < kt.count(); ++x) {
+    const int steps = kt.count();
+    __syncthreads();
+    load_tile<kStep>(sK, K, a.kn, kt.at(0) * kStep, len);
+    load_tile<kStep>(sV, V, a.kn, kt.at(0) * kStep, len);
+    for (int x = 0; x < steps; ++x) {
         const int k0 = kt.at(x) * kStep;
-        __syncthreads();
-        load_tile<kStep>(sK, K, a.kn, k0, len);
-        load_tile<kStep>(sV, V, a.kn, k0, len);
+        const float* keys = sK + (x & 1) * kStep * kLd;
         cp_wait<0>();
         __syncthreads();
+        if (x + 1 < steps) load_tile<kStep>(sK + (~x & 1) * kStep * kLd, K, a.kn, kt.at(x + 1) * kStep, len);
         const bool whole = sees_all(row0, kTile, k0, kStep, a.window, a.sinks);
-        // rows: keys; columns: queries
-        float ds[4][8];
-        f2 d[4][8];
-        dot_half<kLd, kLd>(d, sK, sQ, 16, 0, ry, cx);
+        // rows: keys ry + 8 i; columns: queries 32 half + cx + 8 j
+        float ds[4][4];
+        f2 d[4][4];
+        dot_quarter(d, keys, sQ + 32 * half * kLd, ry, cx);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float base = s_lse[cx + 8 * j];
+        for (int j = 0; j < 4; ++j) {
+            const int r = 32 * half + cx + 8 * j;
+            const float base = s_lse[r];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const bool v = whole || sees(row0 + cx + 8 * j, k0 + ry + 8 * i, a.window, a.sinks);
+                const bool v = whole || sees(row0 + r, k0 + ry + 8 * i, a.window, a.sinks);
                 ds[i][j] = v ? exp2_approx(fmaf(sum2(d[i][j]), a.c, -base)) : 0.f;
             }
         }
-        dot_half<kLd, kLd>(d, sV, sG, 16, 0, ry, cx);
-        __syncthreads();                                  // everyone has read the values
+        dot_quarter(d, sV, sG + 32 * half * kLd, ry, cx);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float D = s_D[cx + 8 * j];
+        for (int j = 0; j < 4; ++j) {
+            const int r = 32 * half + cx + 8 * j;
+            const float D = s_D[r];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const bool v = whole || sees(row0 + cx + 8 * j, k0 + ry + 8 * i, a.window, a.sinks);
-                sP[(ry + 8 * i) * kLd + cx + 8 * j] = v ? ds[i][j] * (sum2(d[i][j]) - D) : 0.f;
+                const bool v = whole || sees(row0 + r, k0 + ry + 8 * i, a.window, a.sinks);
+                sP[(ry + 8 * i) * kLd + r] = v ? ds[i][j] * (sum2(d[i][j]) - D) : 0.f;
             }
         }
-        __syncthreads();
-        outer_product(acc, sP, sK, kStep, kLd, ry, cx);
+        __syncthreads();                                  // (and everyone has read the values)
+        if (x + 1 < steps) load_tile<kStep>(sV, V, a.kn, kt.at(x + 1) * kStep, len);
+        acc.add(sP, keys + col, kStep, ry);
     }
-    s_bad[tid] = 0;
+    if (tid < kTile) s_bad[tid] = 0;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int r = out_row(ry, i);
-        float o[8];
-        const bool nan = s_lse[r] != s_lse[r] || s_D[r] != s_D[r], fine = row_out(acc, i, a.scale, o) || nan;      // (nan: then so is the row)
-        if (row0 + r < end) store_row(dQ + (int64_t)(row0 + r) * a.qn, cx, o);
-        if (cx == 0 && !fine) s_bad[r] = 1;
+        float o[4];
+        const bool nan = s_lse[r] != s_lse[r] || s_D[r] != s_D[r], fine = acc.row(i, a.scale, o) || nan;      // (nan: then so is the row)
+        if (row0 + r < end) store_row(dQ + (int64_t)(row0 + r) * a.qn + col, o);
+        if (!fine) s_bad[r] = 1;
     }
     __syncthreads();
     for (int r = tid / 32; row0 + r < end && r < kTile; r += kThreads / 32)
@@ -308,14 +364,14 @@ constexpr size_t kDkvSmem = 4 * kUnit * sizeof(float);
 
 // The gradients of 64 keys and values: sums over the query rows that see them, head by head of those that share them (a fixed order).
 template <typename T>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 3)
 win_dkv_kernel(const __grid_constant__ WinArgs a) {
     pdl_sync();
     extern __shared__ float sm[];
     __shared__ float s_D[kStep], s_lse[kStep];
     __shared__ int s_bad[kTile];
     float *sK = sm, *sV = sm + kUnit, *sQ = sm + 2 * kUnit, *sG = sQ + kStep * kLd, *sP = sm + 3 * kUnit, *sS = sP + kStep * kLd;
-    const int tid = threadIdx.x, ry = tid / 8, cx = tid % 8;
+    const int tid = threadIdx.x, half = tid / 64, ry = tid % 64 / 8, cx = tid % 8, col = 32 * half + 4 * cx;
     const int tiles = (a.n + kTile - 1) / kTile;
     const KeyItem it = key_item(a, blockIdx.x, kTile, [&](int x) { return x / tiles; }, [&](int x) { return x / a.Hkv; },
                                 [&](int x) { return x / a.parts; });
@@ -331,7 +387,7 @@ win_dkv_kernel(const __grid_constant__ WinArgs a) {
     const int row_end = it.end(a, kTile);
     load_tile(sK, (const T*)a.K + koff, a.kn, key0, end);
     load_tile(sV, (const T*)a.V + koff, a.kn, key0, end);
-    Acc ak, av;
+    HalfAcc ak, av;
     ak.zero();
     av.zero();
     for (int g = 0; g < a.G; ++g) {
@@ -342,61 +398,65 @@ win_dkv_kernel(const __grid_constant__ WinArgs a) {
             __syncthreads();
             load_tile<kStep>(sQ, Q, a.qn, i0, len);
             load_tile<kStep>(sG, dO, a.qn, i0, len);
-            const int si = i0 + tid % kStep;
-            (tid < kStep ? s_lse : s_D)[tid % kStep] = si < len ? -(tid < kStep ? a.stat_l : a.stat_d)[soff + si] : 0.f;
+            if (tid < 2 * kStep) {
+                const int si = i0 + tid % kStep;
+                (tid < kStep ? s_lse : s_D)[tid % kStep] = si < len ? -(tid < kStep ? a.stat_l : a.stat_d)[soff + si] : 0.f;
+            }
             cp_wait<0>();
             __syncthreads();
             const bool whole = i0 + kStep <= len && key0 + kTile - 1 <= i0 && (i0 + kStep - 1 - key0 < a.window || key0 + kTile <= a.sinks);
-            // rows: queries; columns: keys
-            f2 d[4][8];
-            float p[4][8];
-            dot_half<kLd, kLd>(d, sQ, sK, 16, 0, ry, cx);
+            // rows: queries ry + 8 i; columns: keys 32 half + cx + 8 j
+            f2 d[4][4];
+            float p[4][4];
+            dot_quarter(d, sQ, sK + 32 * half * kLd, ry, cx);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int r = ry + 8 * i;
                 const float base = s_lse[r];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const bool v = whole || (i0 + r < len && sees(i0 + r, key0 + cx + 8 * j, a.window, a.sinks));
+                for (int j = 0; j < 4; ++j) {
+                    const int c = 32 * half + cx + 8 * j;
+                    const bool v = whole || (i0 + r < len && sees(i0 + r, key0 + c, a.window, a.sinks));
                     p[i][j] = v ? exp2_approx(fmaf(sum2(d[i][j]), a.c, -base)) : 0.f;
-                    sP[r * kLd + cx + 8 * j] = p[i][j];
+                    sP[r * kLd + c] = p[i][j];
                 }
             }
-            dot_half<kLd, kLd>(d, sG, sV, 16, 0, ry, cx);
+            dot_quarter(d, sG, sV + 32 * half * kLd, ry, cx);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int r = ry + 8 * i;
                 const float D = s_D[r];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const bool v = whole || (i0 + r < len && sees(i0 + r, key0 + cx + 8 * j, a.window, a.sinks));
-                    sS[r * kLd + cx + 8 * j] = v ? p[i][j] * (sum2(d[i][j]) - D) : 0.f;
+                for (int j = 0; j < 4; ++j) {
+                    const int c = 32 * half + cx + 8 * j;
+                    const bool v = whole || (i0 + r < len && sees(i0 + r, key0 + c, a.window, a.sinks));
+                    sS[r * kLd + c] = v ? p[i][j] * (sum2(d[i][j]) - D) : 0.f;
                 }
             }
             __syncthreads();
-            outer_product(av, sP, sG, kStep, kLd, ry, cx);
-            outer_product(ak, sS, sQ, kStep, kLd, ry, cx);
+            av.add(sP, sG + col, kStep, ry);
+            ak.add(sS, sQ + col, kStep, ry);
         }
     }
-    s_bad[tid] = 0;
+    if (tid < kTile) s_bad[tid] = 0;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int r = out_row(ry, i);
-        float k[8], v[8];
-        const bool fk = row_out(ak, i, a.scale, k), fv = row_out(av, i, 1.f, v), fine = fk && fv;
+        float k[4], v[4];
+        const bool fk = ak.row(i, a.scale, k), fv = av.row(i, 1.f, v), fine = fk && fv;
         // (a part's sums stay as they are: each of its pairs counts)
         if (key0 + r < end) {
             if (it.part <= 0) {
-                store_row(dK + (int64_t)(key0 + r) * a.kn, cx, k);
-                store_row(dV + (int64_t)(key0 + r) * a.kn, cx, v);
+                store_row(dK + (int64_t)(key0 + r) * a.kn + col, k);
+                store_row(dV + (int64_t)(key0 + r) * a.kn + col, v);
             }
             if (it.part >= 0 && r < a.sinks) {
-                store_row(partial_row(a, it.b, it.h, it.part, 0, r), cx, k);
-                store_row(partial_row(a, it.b, it.h, it.part, 1, r), cx, v);
+                store_row(partial_row(a, it.b, it.h, it.part, 0, r) + col, k);
+                store_row(partial_row(a, it.b, it.h, it.part, 1, r) + col, v);
             }
         }
-        if (cx == 0 && !fine && it.part <= 0) s_bad[r] = 1;
+        if (!fine && it.part <= 0) s_bad[r] = 1;
     }
     __syncthreads();
     for (int r = tid / 32; key0 + r < end && r < kTile; r += kThreads / 32)
