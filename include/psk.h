@@ -274,7 +274,7 @@ int psk_decode_step(const psk_shape* shape, const void* q, const void* k, const 
  *   workspace     DEVICE scratch for the backward, 16-byte aligned, >= psk_layer_norm_workspace_bytes(shape)
  *                 (0 for a bad shape); not read if dgain and dbias are NULL
  * cols from 1 to 8192, fewer than 2^31 rows.  fp32 arithmetic.  No alignment is asked for: rows that do not lie on 16 bytes
- * are read value by value. */
+ * are read by two values or by one. */
 typedef struct {
     int32_t n0, n1, n2, cols;
     int32_t dtype;              /* psk_dtype */

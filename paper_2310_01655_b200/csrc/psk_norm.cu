@@ -56,7 +56,7 @@ __device__ __forceinline__ float vat(float a, int) { return a; }
 __device__ __forceinline__ void vset(float& a, float v) { a = v; }
 __device__ __forceinline__ void vload(float& a, const float* p) { a = p[0]; }
 
-// V values at p: 16 bytes, or one value
+// V values at p: 16 bytes, two values, or one
 template <typename T, int V> struct Pack;
 template <> struct Pack<float, 4> {
     float4 v;
@@ -79,6 +79,24 @@ template <> struct Pack<bf16, 8> {
 #pragma unroll
         for (int i = 0; i < 4; ++i) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(u[i]) : "f"(hi2(f[i])), "f"(lo2(f[i])));
         *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
+    }
+};
+template <> struct Pack<float, 2> {
+    float2 v;
+    __device__ __forceinline__ void load(const float* p) { v = *reinterpret_cast<const float2*>(p); }
+    __device__ __forceinline__ void zero() { v = make_float2(0.f, 0.f); }
+    __device__ __forceinline__ void get(f2* f) const { f[0] = pack2(v.x, v.y); }
+    __device__ __forceinline__ static void store(float* p, const f2* f) { *reinterpret_cast<float2*>(p) = make_float2(lo2(f[0]), hi2(f[0])); }
+};
+template <> struct Pack<bf16, 2> {
+    uint32_t v;
+    __device__ __forceinline__ void load(const bf16* p) { v = *reinterpret_cast<const uint32_t*>(p); }
+    __device__ __forceinline__ void zero() { v = 0u; }
+    __device__ __forceinline__ void get(f2* f) const { f[0] = pack2(v << 16, v & 0xffff0000u); }
+    __device__ __forceinline__ static void store(bf16* p, const f2* f) {
+        uint32_t u;
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(u) : "f"(hi2(f[0])), "f"(lo2(f[0])));
+        *reinterpret_cast<uint32_t*>(p) = u;
     }
 };
 template <typename T> struct Pack<T, 1> {
@@ -122,7 +140,7 @@ __device__ __forceinline__ float over_cols(const NormArgs& a, float s) {
 template <int V, int NV, int G> struct RowMap {
     static constexpr int kRowsPerCta = kNormThreads / G, kPer = (V + 1) / 2, kPairs = kPer * NV, kValues = V * NV;
     // rows in flight per lane, as registers allow
-    static constexpr int kFwdRows = kValues <= 8 ? 4 : (kValues <= 16 ? 4 : 3), kBwdRows = kValues <= 16 ? 2 : 1;
+    static constexpr int kFwdRows = kValues <= 8 ? 4 : (kValues <= 16 ? 4 : 3), kBwdRows = kValues <= (V == 1 ? 8 : 16) ? 2 : 1;
 };
 // a parameter's values at the lane's columns (1 or 0 where there is none)
 template <int V> __device__ __forceinline__ void load_param(typename Word<V>::type* f, const float* p, int vec, bool in, float none) {
@@ -391,8 +409,6 @@ norm_sum_kernel(const float* __restrict__ partial, int parts, int cols, float* _
 
 constexpr int kNormMaxCtas = 148 * 2;           // (with rows in flight two per SM are enough, and fewer sums are left to add up)
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
 // extents and strides in the order of X's strides, so that neighbouring rows are read together
 struct Order { int32_t n[3]; int idx[3]; };
 Order order_of(const psk_norm_shape* sh) {
@@ -462,10 +478,19 @@ cudaError_t launch(const NormArgs& a, bool backward, cudaStream_t s) {
 }
 
 template <typename T>
-cudaError_t dispatch(const NormArgs& a, bool vec, bool backward, cudaStream_t s) {
+cudaError_t dispatch(const NormArgs& a, int width, bool backward, cudaStream_t s) {
     constexpr int V = 16 / sizeof(T);
-    const int nvec = vec ? a.cols / V : a.cols;
-    if (!vec) {
+    const int nvec = a.cols / width;
+    if (width == 2) {                     // (65 536 rows of 1002, bf16, us by twos / one by one: forward 87 / 101, backward 134 / 154; 16 384 of 3002: 68 / 115, 111 / 410)
+        if (nvec <= 32) return launch<T, 2, 1, 32>(a, backward, s);
+        if (nvec <= 128) return launch<T, 2, 4, 32>(a, backward, s);
+        if (nvec <= 256) return launch<T, 2, 4, 64>(a, backward, s);
+        if (nvec <= 512) return launch<T, 2, 4, 128>(a, backward, s);
+        if (nvec <= 1024) return launch<T, 2, 4, 256>(a, backward, s);
+        if (nvec <= 2048) return launch<T, 2, 8, 256>(a, backward, s);
+        return launch<T, 2, 16, 256>(a, backward, s);
+    }
+    if (width == 1) {
         if (nvec <= 32) return launch<T, 1, 1, 32>(a, backward, s);
         if (nvec <= 128) return launch<T, 1, 4, 32>(a, backward, s);
         if (nvec <= 256) return launch<T, 1, 8, 32>(a, backward, s);
@@ -497,18 +522,24 @@ int run(const psk_norm_shape* sh, NormArgs& a, bool backward, cudaStream_t s) {
     a.over_cols = 1.f / (float)sh->cols;
     a.n1.set((uint32_t)o.n[1]);
     a.n2.set((uint32_t)o.n[2]);
-    const int per = sh->dtype == PSK_F32 ? 4 : 8;
-    bool vec = sh->cols % per == 0;
-    for (const void* p : {a.x, a.y, (const void*)a.z}) vec = vec && aligned16(p);
+    // values that every row can be read by at once: 16 bytes' worth, two, or one
+    const int esz = sh->dtype == PSK_F32 ? 4 : 2;
+    int width = 16 / esz;
+    auto whole = [&](int64_t values, uintptr_t bytes) {
+        while (width > 1 && (values % width != 0 || bytes % (uintptr_t)(width * esz) != 0)) width = width > 2 ? 2 : 1;
+    };
+    whole(sh->cols, 0);
+    for (const void* p : {a.x, a.y, (const void*)a.z}) whole(0, reinterpret_cast<uintptr_t>(p));
     const int64_t* in = sh->xs;
     for (int i = 0; i < 3; ++i) {
         const int k = o.idx[i];
         a.xs[i] = in[k];
         a.ys[i] = backward ? sh->ys[k] : 0;
         a.zs[i] = backward ? sh->zs[k] : sh->ys[k];
-        if (o.n[i] > 1) vec = vec && a.xs[i] % per == 0 && a.ys[i] % per == 0 && a.zs[i] % per == 0;
+        if (o.n[i] > 1)
+            for (int64_t v : {a.xs[i], a.ys[i], a.zs[i]}) whole(v, 0);
     }
-    const cudaError_t e = sh->dtype == PSK_F32 ? dispatch<float>(a, vec, backward, s) : dispatch<bf16>(a, vec, backward, s);
+    const cudaError_t e = sh->dtype == PSK_F32 ? dispatch<float>(a, width, backward, s) : dispatch<bf16>(a, width, backward, s);
     return e == cudaSuccess ? PSK_OK : PSK_ERR_CUDA;
 }
 

@@ -127,6 +127,29 @@ def test_rows_off_16_bytes(dtype):
     assert torch.equal(psk.layer_norm_fwd(flat, gain, out=torch.empty(3, 64, dtype=X.dtype, device="cuda")), psk.layer_norm_fwd(flat, gain))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols,stride,start", [(1, 2, 2, 0), (300, 6, 6, 2), (77, 64, 70, 2), (50, 130, 130, 0), (40, 254, 256, 2), (31, 258, 262, 4), (20, 514, 514, 6),
+                                                    (33, 1002, 1002, 0), (9, 1026, 1030, 2), (7, 2046, 2050, 0), (6, 2050, 2050, 0), (5, 4094, 4094, 2), (4, 4098, 4098, 0),
+                                                    (3, 8190, 8190, 2), (2, 8192, 8194, 2), (2000, 90, 90, 0)])
+def test_rows_on_two_values(dtype, rows, cols, stride, start):
+    """Even columns, strides and starts that are not whole 16 bytes."""
+    def make(seed, offset=0.0):
+        flat = torch.zeros(start + rows * stride + 8, dtype=DT[dtype], device="cuda")
+        x = flat[start:start + rows * stride].view(rows, stride)[:, :cols]
+        x.copy_(rows_of(dtype, rows, cols, seed=seed, offset=offset))
+        return flat, x
+    (fx, X), (fd, dY), (fo, out) = make(cols), make(cols + 1, 0.1), make(3)
+    gain, bias = 1 + 0.1 * rows_of("f32", cols, seed=3), rows_of("f32", cols, seed=4)
+    between = torch.ones_like(fo, dtype=torch.bool)
+    between[start:start + rows * stride].view(rows, stride)[:, :cols] = False
+    before = fo.clone()
+    Y = psk.layer_norm_fwd(X, gain, bias, out=out).clone()
+    assert torch.equal(fo[between], before[between])
+    dX, dgain, dbias = psk.layer_norm_bwd(X, gain, dY, out=out)
+    assert torch.equal(fo[between], before[between])
+    check(dtype, X, gain, bias, dY, Y, dX, dgain, dbias)
+
+
 def test_large_offsets_and_constant_rows():
     # a mean a thousand times the spread; rows without any spread: eps alone is under the root
     X = rows_of("f32", 64, 768, seed=8) + 1000.0
