@@ -363,10 +363,12 @@ win_dq_kernel(const __grid_constant__ WinArgs a) {
 constexpr size_t kDkvSmem = 4 * kUnit * sizeof(float);
 
 // The gradients of 64 keys and values: sums over the query rows that see them, head by head of those that share them (a fixed order).
-template <typename T>
+// SPLIT 1: there are items that are parts of the sinks' tiles; 2: that, or key heads in several
+template <typename T, int SPLIT>
 __global__ void __launch_bounds__(kThreads, 3)
 win_dkv_kernel(const __grid_constant__ WinArgs a) {
     pdl_sync();
+    const int hs = SPLIT == 2 ? a.hs : 1;
     extern __shared__ float sm[];
     __shared__ float s_D[kStep], s_lse[kStep];
     __shared__ int s_bad[kTile];
@@ -375,10 +377,10 @@ win_dkv_kernel(const __grid_constant__ WinArgs a) {
     const int tiles = (a.n + kTile - 1) / kTile;
     const KeyItem it = key_item(a, blockIdx.x, kTile, [&](int x) { return x / tiles; }, [&](int x) { return x / a.Hkv; },
                                 [&](int x) { return x / a.parts; });
-    const int64_t koff = it.b * a.kb + it.h * a.kh;
+    const int64_t koff = it.b * a.kb + it.h / hs * a.kh;
     T *dK = (T*)a.dK + koff, *dV = (T*)a.dV + koff;
     const int key0 = it.key0, len = it.len, n_end = key0 + kTile < a.n ? key0 + kTile : a.n, end = key0 + kTile < len ? key0 + kTile : len;
-    if (it.part <= 0) {
+    if ((SPLIT == 0 || it.part <= 0) && hs == 1) {
         const int none = end > key0 ? end - key0 : 0;
         zero_rows(dK + (int64_t)none * a.kn, a.kn, key0, n_end - none);
         zero_rows(dV + (int64_t)none * a.kn, a.kn, key0, n_end - none);
@@ -447,25 +449,33 @@ win_dkv_kernel(const __grid_constant__ WinArgs a) {
         const bool fk = ak.row(i, a.scale, k), fv = av.row(i, 1.f, v), fine = fk && fv;
         // (a part's sums stay as they are: each of its pairs counts)
         if (key0 + r < end) {
-            if (it.part <= 0) {
+            if ((SPLIT == 0 || it.part <= 0) && hs == 1) {
                 store_row(dK + (int64_t)(key0 + r) * a.kn + col, k);
                 store_row(dV + (int64_t)(key0 + r) * a.kn + col, v);
+            } else if ((SPLIT == 0 || it.part <= 0)) {
+                store_row(sum_row(a, it.b, it.h, 0, key0 + r) + col, k);
+                store_row(sum_row(a, it.b, it.h, 1, key0 + r) + col, v);
             }
-            if (it.part >= 0 && r < a.sinks) {
+            if (SPLIT > 0 && it.part >= 0 && r < a.sinks) {
                 store_row(partial_row(a, it.b, it.h, it.part, 0, r) + col, k);
                 store_row(partial_row(a, it.b, it.h, it.part, 1, r) + col, v);
             }
         }
-        if (!fine && it.part <= 0) s_bad[r] = 1;
+        if (!fine && (SPLIT == 0 || it.part <= 0)) s_bad[r] = 1;
     }
     __syncthreads();
     for (int r = tid / 32; key0 + r < end && r < kTile; r += kThreads / 32)
         if (s_bad[r] && key_tainted<T>(a, it.b, it.h, key0 + r, len, it.stop)) {
             const int c = 2 * (tid % 32);
-            const bool sum = it.part == 0 && r < a.sinks;
+            const bool sum = SPLIT > 0 && it.part == 0 && r < a.sinks;
             const KeyRow k = redo_dkv_row<T>(a, it.b, it.h, key0 + r, len, sum ? row_end : len);
-            st2(dK + (int64_t)(key0 + r) * a.kn + c, k.dk);
-            st2(dV + (int64_t)(key0 + r) * a.kn + c, k.dv);
+            if (hs == 1) {
+                st2(dK + (int64_t)(key0 + r) * a.kn + c, k.dk);
+                st2(dV + (int64_t)(key0 + r) * a.kn + c, k.dv);
+            } else {
+                st2(sum_row(a, it.b, it.h, 0, key0 + r) + c, k.dk);
+                st2(sum_row(a, it.b, it.h, 1, key0 + r) + c, k.dv);
+            }
             if (sum) {
                 st2(partial_row(a, it.b, it.h, 0, 0, r) + c, k.dk);
                 st2(partial_row(a, it.b, it.h, 0, 1, r) + c, k.dv);
@@ -490,6 +500,32 @@ win_sink_sum_kernel(const __grid_constant__ WinArgs a) {
     }
 }
 
+// The gradients of keys and values whose query heads were dealt to several (the sinks' from their parts): four columns of a row to a thread.
+template <typename T>
+__global__ void __launch_bounds__(256)
+win_head_sum_kernel(const __grid_constant__ WinArgs a) {
+    pdl_sync();
+    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;             // [B, real key head, dK/dV, row, 16 x 4 columns]
+    const int c = (int)(e % 16) * 4;
+    const int64_t row = e / 16;
+    const int j = (int)(row % a.n), which = (int)(row / a.n % 2), heads = a.Hkv / a.hs;
+    const int64_t bh = row / a.n / 2;
+    if (bh >= (int64_t)a.B * heads) return;
+    const int b = (int)(bh / heads), hk = (int)(bh % heads), len = length_of(a, b);
+    float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](const float* p) {
+        const float4 v = *reinterpret_cast<const float4*>(p + c);
+        t.x += v.x; t.y += v.y; t.z += v.z; t.w += v.w;
+    };
+    if (j < len)
+        for (int h = hk * a.hs; h < (hk + 1) * a.hs; ++h) {
+            if (a.parts == 0 || j >= a.sinks) { add(sum_row(a, b, h, which, j)); continue; }
+            add(partial_row(a, b, h, 0, which, j));
+            for (int q = 0; q < a.parts && a.split_row + q * a.part_rows < len; ++q) add(partial_row(a, b, h, q + 1, which, j));
+        }
+    store4((T*)(which ? a.dV : a.dK) + b * a.kb + hk * a.kh + (int64_t)j * a.kn + c, t.x, t.y, t.z, t.w);
+}
+
 template <typename Kern>
 cudaError_t launch_rows(const char* name, Kern kern, size_t smem, unsigned grid, const WinArgs& a, cudaStream_t s) {
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
@@ -505,12 +541,20 @@ cudaError_t cc_window_fwd(const WinArgs& a, cudaStream_t s) {
     return launch_rows("win_fwd_kernel", win_fwd_kernel<T>, kFwdSmem, tiles * a.B * a.H, a, s);
 }
 template <typename T>
-cudaError_t cc_window_bwd(const WinArgs& a, cudaStream_t s) {
+cudaError_t cc_window_bwd(const WinArgs& a, const WinArgs& k, cudaStream_t s) {
     const unsigned tiles = (unsigned)((a.n + kTile - 1) / kTile);
     const cudaError_t e = launch_rows("win_dq_kernel", win_dq_kernel<T>, kDqSmem, tiles * a.B * a.H, a, s);
-    return e != cudaSuccess ? e : launch_rows("win_dkv_kernel", win_dkv_kernel<T>, kDkvSmem, (tiles + a.parts) * a.B * a.Hkv, a, s);
+    return e != cudaSuccess ? e : launch_rows("win_dkv_kernel", k.hs > 1 ? win_dkv_kernel<T, 2> : k.parts > 0 ? win_dkv_kernel<T, 1> : win_dkv_kernel<T, 0>, kDkvSmem, (tiles + k.parts) * k.B * k.Hkv, k, s);
 }
-cudaError_t sink_sum(const WinArgs& a, bool half, cudaStream_t s) {
+cudaError_t key_sums(const WinArgs& a, bool half, cudaStream_t s) {
+    if (a.hs > 1) {
+        const int64_t grid = ((int64_t)a.B * (a.Hkv / a.hs) * a.n * 32 + 255) / 256;
+        prof_begin("win_head_sum_kernel", s);
+        if (half) launch_pdl(win_head_sum_kernel<bf16>, dim3((unsigned)grid), dim3(256), 0, s, a);
+        else launch_pdl(win_head_sum_kernel<float>, dim3((unsigned)grid), dim3(256), 0, s, a);
+        prof_end(s);
+        return cudaGetLastError();
+    }
     if (a.parts == 0) return cudaSuccess;
     prof_begin("win_sink_sum_kernel", s);
     if (half) launch_pdl(win_sink_sum_kernel<bf16>, dim3(a.B * a.Hkv, (a.sinks + 1) / 2), dim3(256), 0, s, a);
@@ -559,7 +603,7 @@ int check_rows(const psk_window_shape* sh) {
     st = check_strides(sh->B, sh->H, sh->n, sh->q_stride_b, sh->q_stride_h, sh->q_stride_n, esz);
     return st != PSK_OK ? st : check_strides(sh->B, sh->Hkv, sh->n, sh->kv_stride_b, sh->kv_stride_h, sh->kv_stride_n, esz);
 }
-void plan_parts(WinArgs& a, int tile) {
+static void plan_parts(WinArgs& a, int tile) {
     a.parts = a.part_rows = a.split_row = 0;
     if (a.sinks == 0 || a.sinks > tile) return;
     const int64_t split = ((int64_t)tile + a.window - 1 + 63) / 64 * 64;               // rows before it see more than the sinks
@@ -573,6 +617,23 @@ void plan_parts(WinArgs& a, int tile) {
     a.part_rows = (int)((rest + parts - 1) / parts * 64);
     a.parts = (int)((a.n - split + a.part_rows - 1) / a.part_rows);
 }
+WinArgs key_side(const WinArgs& a, int tile) {
+    WinArgs k = a;
+    k.hs = 1;
+    // Places that the GPU has for CTAs, and the least rows of an item that are worth the sum behind it (a step of 64 rows takes the tensor cores
+    // 0.8 us, the CUDA cores up to 18; the sum 4 to 10).  8 query heads x 2000 rows on one key head, window 500, us: bf16 61 -> 19 + 7, fp32 846 -> 173 + 8.
+    const int64_t items = ((int64_t)a.n + tile - 1) / tile * a.B * a.Hkv, places = tile == 128 ? 148 : 444, least = (tile == 128 ? 24 : 4) * 64;
+    const int64_t seen = (int64_t)a.window + tile < a.n ? (int64_t)a.window + tile : a.n;
+    if (items < places && a.G > 1 && seen * a.G >= least)
+        for (k.hs = 2; k.hs < a.G && (a.G % k.hs != 0 || items * k.hs < places); ++k.hs) {}
+    k.Hkv *= k.hs;
+    k.G /= k.hs;
+    plan_parts(k, tile);
+    return k;
+}
+// Bytes of the sums over query heads and over parts.
+static size_t row_sum_bytes(const WinArgs& k) { return k.hs > 1 ? (size_t)k.B * k.Hkv * k.n * 2 * 64 * sizeof(float) : 0; }
+static size_t partial_bytes(const WinArgs& k) { return k.parts > 0 ? (size_t)k.B * k.Hkv * (k.parts + 1) * 2 * k.sinks * 64 * sizeof(float) : 0; }
 static bool on_tensor_cores(const psk_window_shape* sh) { return sh->dtype == PSK_BF16 && sh->path != PSK_PATH_CUDA_CORES; }
 // Device waits are bounded by a second, and some last as long as a tile: 2^25 rows of query heads on one tile of keys take the key side 0.4 s.
 static int check_attention(const psk_window_shape* sh) {
@@ -583,6 +644,7 @@ static int check_attention(const psk_window_shape* sh) {
 }
 WinArgs args_of(const psk_window_shape* sh) {
     WinArgs a{};
+    a.hs = 1;
     a.B = sh->B; a.H = sh->H; a.Hkv = sh->Hkv; a.G = sh->H / sh->Hkv; a.n = sh->n;
     a.window = sh->window; a.sinks = sh->sinks;
     a.scale = sh->scale; a.c = sh->scale * kLog2e;
@@ -603,14 +665,14 @@ extern "C" {
 size_t psk_window_workspace_bytes(const psk_window_shape* shape, int for_backward) {
     if (check_attention(shape) != PSK_OK) return 0;
     if (!for_backward) return kStatusBytes;
-    WinArgs a = args_of(shape);
-    size_t parts = 0;                                     // (enough for either path)
+    const WinArgs a = args_of(shape);
+    size_t sums = 0;                                      // (enough for either path)
     for (int tile = kTile; tile <= 128; tile += 64) {
-        plan_parts(a, tile);
-        const size_t bytes = a.parts > 0 ? align_up((size_t)a.B * a.Hkv * (a.parts + 1) * 2 * a.sinks * 64 * sizeof(float)) : 0;
-        if (bytes > parts) parts = bytes;
+        const WinArgs k = key_side(a, tile);
+        const size_t bytes = align_up(row_sum_bytes(k)) + align_up(partial_bytes(k));
+        if (bytes > sums) sums = bytes;
     }
-    return kStatusBytes + 2 * align_up((size_t)a.B * a.H * a.n * sizeof(float)) + parts;
+    return kStatusBytes + 2 * align_up((size_t)a.B * a.H * a.n * sizeof(float)) + sums;
 }
 
 int psk_window_attn_fwd(const psk_window_shape* shape, const void* Q, const void* K, const void* V, const int32_t* lengths, void* O, float* lse,
@@ -650,17 +712,18 @@ int psk_window_attn_bwd(const psk_window_shape* shape, const void* Q, const void
     a.Q = Q; a.K = K; a.V = V; a.O = O; a.lse_in = lse; a.dO = dO; a.dQ = dQ; a.dK = dK; a.dV = dV; a.lengths = lengths;
     a.stat_l = reinterpret_cast<float*>(static_cast<char*>(workspace) + kStatusBytes);
     a.stat_d = a.stat_l + align_up((size_t)a.B * a.H * a.n * sizeof(float)) / sizeof(float);
-    a.partial = a.stat_d + align_up((size_t)a.B * a.H * a.n * sizeof(float)) / sizeof(float);
-    plan_parts(a, on_tensor_cores(shape) ? 128 : kTile);
+    WinArgs k = key_side(a, on_tensor_cores(shape) ? 128 : kTile);
+    k.rows = a.stat_d + align_up((size_t)a.B * a.H * a.n * sizeof(float)) / sizeof(float);
+    k.partial = k.rows + align_up(row_sum_bytes(k)) / sizeof(float);
     int* status = static_cast<int*>(workspace);
     cudaError_t e;
     if (on_tensor_cores(shape)) {
-        e = tc_window_bwd(a, status, s);
+        e = tc_window_bwd(a, k, status, s);
     } else {
         a.status = status;
-        e = shape->dtype == PSK_F32 ? cc_window_bwd<float>(a, s) : cc_window_bwd<bf16>(a, s);
+        e = shape->dtype == PSK_F32 ? cc_window_bwd<float>(a, k, s) : cc_window_bwd<bf16>(a, k, s);
     }
-    if (e == cudaSuccess) e = sink_sum(a, shape->dtype == PSK_BF16, s);
+    if (e == cudaSuccess) e = key_sums(k, shape->dtype == PSK_BF16, s);
     return e == cudaSuccess ? PSK_OK : PSK_ERR_CUDA;
 }
 

@@ -28,7 +28,14 @@ struct WinArgs {
     // `partial` [B Hkv][parts + 1][dK, dV][sinks][64] in a fixed order (part 0: the rows before split_row).  parts = 0: nothing of that.
     int parts, part_rows, split_row;
     float* partial;
+    // Key side: where key heads and tiles are too few for the GPU, the query heads that share a key head are dealt to `hs` heads that do as
+    // if they were key heads of their own (Hkv and G there: times and through hs); their sums are added up from `rows` [B Hkv][dK, dV][n][64].
+    int hs;
+    float* rows;
 };
+__device__ __forceinline__ float* sum_row(const WinArgs& a, int b, int hk, int which, int j) {
+    return a.rows + ((((int64_t)b * a.Hkv + hk) * 2 + which) * a.n + j) * 64;
+}
 __device__ __forceinline__ float* partial_row(const WinArgs& a, int b, int hk, int part, int which, int j) {
     return a.partial + ((((int64_t)b * a.Hkv + hk) * (a.parts + 1) + part) * 2 + which) * a.sinks * 64 + (int64_t)j * 64;
 }
@@ -192,7 +199,7 @@ struct KeyRow { float2 dk, dv; };
 template <typename T>
 __device__ __noinline__ KeyRow redo_dkv_row(const WinArgs& a, int b, int hk, int j, int len, int stop) {
     const int l2 = 2 * (threadIdx.x % 32);
-    const int64_t krow = b * a.kb + hk * a.kh + j * a.kn + l2;
+    const int64_t krow = b * a.kb + hk / a.hs * a.kh + j * a.kn + l2;
     const float2 k = ld2((const T*)a.K + krow), v = ld2((const T*)a.V + krow);
     KeyRow r{make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
     const int64_t past = (int64_t)j + a.window;
@@ -287,12 +294,12 @@ __device__ __forceinline__ KeyItem key_item(const WinArgs& a, int index, int til
 int check_common(const psk_window_shape* sh);         // all but n and the strides
 int check_rows(const psk_window_shape* sh);
 WinArgs args_of(const psk_window_shape* sh);
-void plan_parts(WinArgs& a, int tile);                // fills parts, part_rows, split_row
+WinArgs key_side(const WinArgs& a, int tile);         // as the key side takes them: with hs, parts, part_rows, split_row
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // tensor cores (psk_window_tc.cu): bf16
 cudaError_t tc_window_fwd(const WinArgs& a, int* status, cudaStream_t s);
-cudaError_t tc_window_bwd(const WinArgs& a, int* status, cudaStream_t s);
+cudaError_t tc_window_bwd(const WinArgs& a, const WinArgs& k, int* status, cudaStream_t s);      // k: for the key side
 
 }  // namespace win
 }  // namespace psk

@@ -757,7 +757,7 @@ struct Dkv {
     static constexpr uint32_t kTmem = 512, cDk = 0, cDv = 64, cS = 128;        // cS + 128 warpgroup: S (p), dP (ds)
 };
 
-// PARTS: there are items that are parts of the sinks' tiles (the code for them costs others 4 %: 699 against 674 us on 8192 rows of 16 x 12 heads)
+// PARTS: there are items that are parts of the sinks' tiles, or key heads in several (the code for them costs others 4 %: 699 against 674 us on 8192 rows of 16 x 12 heads)
 template <bool PARTS>
 __global__ void __launch_bounds__(Dkv::kThreads, 1)
 tc_win_dkv_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV, const __grid_constant__ CUtensorMap mapQ,
@@ -812,8 +812,9 @@ tc_win_dkv_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constan
                 ++items;
                 if (elect_one()) {
                     mbar_expect_tx(&bar_kv[kv], 32768);
-                    tma_load_4d(smem + Dkv::KV + kv * 32768, &mapK, 0, p.key0, p.h, p.b, &bar_kv[kv]);
-                    tma_load_4d(smem + Dkv::KV + kv * 32768 + 16384, &mapV, 0, p.key0, p.h, p.b, &bar_kv[kv]);
+                    const int hk = PARTS ? p.h / a.hs : p.h;
+                    tma_load_4d(smem + Dkv::KV + kv * 32768, &mapK, 0, p.key0, hk, p.b, &bar_kv[kv]);
+                    tma_load_4d(smem + Dkv::KV + kv * 32768 + 16384, &mapV, 0, p.key0, hk, p.b, &bar_kv[kv]);
                 }
                 for (int x = 0, h = p.h * a.G, i0 = p.begin; x < steps; ++x, ++t, i0 += 64) {
                     const int s = t % Dkv::kStages;
@@ -968,10 +969,18 @@ tc_win_dkv_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constan
                     ok = mbar_wait(&bar_fin[items & 3], (items / 4) & 1, status, kErrMma) && ok;
                     tc_fence_after();
                     bar_sync(1 + group, kRows);
-                    const bool live = j < p.len, sum = PARTS && p.part >= 0 && row < a.sinks;      // sum: this row's gradients are added up from parts
+                    const bool live = j < p.len;
+                    // where this row's gradients are added up from
+                    auto sum_place = [&](int r) -> float* {
+                        if (p.part >= 0 && r < a.sinks) return partial_row(a, p.b, p.h, p.part, has_k ? 0 : 1, r);
+                        return p.part <= 0 && a.hs > 1 ? sum_row(a, p.b, p.h, has_k ? 0 : 1, p.key0 + r) : nullptr;
+                    };
                     const uint32_t from = lane_tm + (has_k ? Dkv::cDk : Dkv::cDv);
                     const float f = has_k ? a.scale : 1.f;
-                    if (PARTS && __any_sync(0xffffffffu, sum)) store_partial(partial_row(a, p.b, p.h, p.part, has_k ? 0 : 1, row), from, f, ok && sum && live);
+                    if (PARTS) {
+                        float* to = live && ok ? sum_place(row) : nullptr;
+                        if (__any_sync(0xffffffffu, to != nullptr)) store_partial(to, from, f, to != nullptr);
+                    }
                     if (PARTS && p.part > 0) {
                         tc_fence_before();
                         if (lane == 0) mbar_arrive(&bar_acc);
@@ -988,16 +997,16 @@ tc_win_dkv_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constan
                             if (!key_tainted<bf16>(a, p.b, p.h, j_first + k, p.len, p.stop)) continue;
                             const KeyRow key = redo_dkv_row<bf16>(a, p.b, p.h, j_first + k, p.len, part ? p.stop : p.len);
                             stage_pair(st, r, has_k ? key.dk : key.dv);
-                            if (part) st2(partial_row(a, p.b, p.h, 0, has_k ? 0 : 1, r) + 2 * lane, has_k ? key.dk : key.dv);
+                            if (PARTS && sum_place(r) != nullptr) st2(sum_place(r) + 2 * lane, has_k ? key.dk : key.dv);
                         }
                         fence_proxy_async_smem();
                         bar_sync(1 + group, kRows);
-                        if (row == 0 && !cta_gave_up()) { tma_store_4d(has_k ? &mapDk : &mapDv, st, 0, p.key0, p.h, p.b); bulk_commit(); }
+                        if (row == 0 && !cta_gave_up() && (!PARTS || a.hs == 1)) { tma_store_4d(has_k ? &mapDk : &mapDv, st, 0, p.key0, p.h, p.b); bulk_commit(); }
                     }
                 }
                 t0 = end;
                 ++items;
-            } else if (group < 2 && p.part <= 0) {
+            } else if (group < 2 && p.part <= 0 && (!PARTS || a.hs == 1)) {
                 zero_tile<kRows>((bf16*)(group == 0 ? a.dK : a.dV) + p.b * a.kb + p.h * a.kh, a.kn, p.key0, a.n, row);
             }
             index = sched_next(sched, it, status);
@@ -1034,7 +1043,7 @@ cudaError_t tc_window_fwd(const WinArgs& a, int* status, cudaStream_t s) {
     return cudaGetLastError();
 }
 
-cudaError_t tc_window_bwd(const WinArgs& a, int* status, cudaStream_t s) {
+cudaError_t tc_window_bwd(const WinArgs& a, const WinArgs& k, int* status, cudaStream_t s) {
     const unsigned tiles = (unsigned)((a.n + kRows - 1) / kRows);
     {
         CUtensorMap mQ, mG, mO, mK, mV, mDq;
@@ -1049,10 +1058,10 @@ cudaError_t tc_window_bwd(const WinArgs& a, int* status, cudaStream_t s) {
     if (!map_k(a, &mK, a.K, 128) || !map_k(a, &mV, a.V, 128) || !map_q(a, &mQ, a.Q, 64) || !map_q(a, &mG, a.dO, 64) || !map_k(a, &mDk, a.dK, 128) ||
         !map_k(a, &mDv, a.dV, 128))
         return cudaErrorInvalidValue;
-    const auto dkv = a.parts > 0 ? tc_win_dkv_kernel<true> : tc_win_dkv_kernel<false>;
+    const auto dkv = k.parts > 0 || k.hs > 1 ? tc_win_dkv_kernel<true> : tc_win_dkv_kernel<false>;
     PSK_TRY(set_smem(dkv, Dkv::bytes));
     prof_begin("tc_win_dkv_kernel", s);
-    launch_pdl(dkv, dim3((tiles + a.parts) * a.B * a.Hkv), dim3(Dkv::kThreads), Dkv::bytes, s, mK, mV, mQ, mG, mDk, mDv, a, item_map(a, a.Hkv), status);
+    launch_pdl(dkv, dim3((tiles + k.parts) * k.B * k.Hkv), dim3(Dkv::kThreads), Dkv::bytes, s, mK, mV, mQ, mG, mDk, mDv, k, item_map(k, k.Hkv), status);
     prof_end(s);
     return cudaGetLastError();
 }

@@ -197,6 +197,50 @@ def test_masked_infinities_and_nans(dtype, path, bad, window, sinks):
 
 
 @pytest.mark.parametrize("dtype,path", PATHS)
+@pytest.mark.parametrize("B,H,Hkv,n,window,sinks,lengths", [
+    (1, 8, 1, 700, 300, 0, None), (2, 12, 2, 333, 333, 0, [333, 100]), (1, 16, 1, 1500, 200, 3, None), (3, 6, 1, 600, 500, 70, [0, 599, 65]),
+    (1, 10, 2, 513, 2000, 1, [512]), (1, 3, 1, 1111, 600, 0, None), (1, 32, 1, 150, 100, 0, None)])
+def test_few_key_heads(dtype, path, B, H, Hkv, n, window, sinks, lengths):
+    """Many query heads to few key heads: their gradients may be added up from several groups of heads."""
+    Q, K, V, dO = make(dtype, B, H, Hkv, n, seed=n + H)
+    lens = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    out = run(Q, K, V, dO, window, sinks, path=path, lengths=lens)
+    check_heads(dtype, Q, K, V, dO, out, window, sinks, lengths=lengths, heads=[(b, Hkv - 1) for b in range(B)])
+    for b in range(B if lengths else 0):
+        assert all(x[b, :, lengths[b]:].eq(0).all() for x in out[2:])
+    for x, y in zip(out, run(Q, K, V, dO, window, sinks, path=path, lengths=lens)):
+        assert torch.equal(x, y)
+    # keys inside a projection: what lies between them is left as it was
+    both = torch.full((2, B, n, Hkv, 2, 64), 3.0, dtype=DT[dtype], device="cuda")
+    dK, dV = (both[i, :, :, :, i].transpose(1, 2) for i in range(2))
+    K2 = torch.zeros_like(both[0])
+    Ks, Vs = K2[:, :, :, 0].transpose(1, 2), K2[:, :, :, 1].transpose(1, 2)
+    Ks.copy_(K), Vs.copy_(V)
+    psk.window_attn_bwd(Q, Ks, Vs, out[0], out[1], dO, window, sinks, lengths=lens, path=path, out=(torch.empty_like(Q), dK, dV))
+    assert torch.equal(dK, out[3]) and torch.equal(dV, out[4])
+    assert (both[0, :, :, :, 1] == 3).all() and (both[1, :, :, :, 0] == 3).all()
+
+
+@pytest.mark.parametrize("dtype,path", PATHS)
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+@pytest.mark.parametrize("window,sinks", [(200, 0), (150, 40), (2000, 0)])
+def test_few_key_heads_with_infinities(dtype, path, bad, window, sinks):
+    n, s = 700, 333
+    Q, K, V, dO = make(dtype, 1, 8, 1, n, seed=41)
+    Q[0, 5, s] = bad                       # one query row of one of the eight heads
+    got = run(Q, K, V, dO, window, sinks, path=path)
+    clean = make(dtype, 1, 8, 1, n, seed=41)
+    good = run(clean[0], K, V, dO, window, sinks, path=path)
+    seen = torch.zeros(n, dtype=torch.bool, device="cuda")
+    seen[max(0, s - window + 1):s + 1] = True
+    seen[:min(sinks, s + 1)] = True
+    for x, y in zip(got[3:], good[3:]):
+        assert not torch.isfinite(x[0, 0, seen].float()).any() and torch.isfinite(x[0, 0, ~seen].float()).all()
+        a, b = x[0, 0, ~seen].double(), y[0, 0, ~seen].double()
+        assert (a - b).norm() <= 4 * max(E[dtype], 1e-6) * b.norm()
+
+
+@pytest.mark.parametrize("dtype,path", PATHS)
 @pytest.mark.parametrize("bad", [float("inf"), float("nan")])
 @pytest.mark.parametrize("which", ["q row", "k row", "k", "v", "dO", "all"])
 @pytest.mark.parametrize("window,sinks", [(70, 0), (60, 130), (2000, 0)])
