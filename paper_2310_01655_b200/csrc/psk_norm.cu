@@ -432,7 +432,7 @@ bool rows_apart(const int32_t (&n)[3], const int64_t* s, int cols) {
             if (!used[i] && n[i] > 1 && (at < 0 || s[i] < s[at])) at = i;
         if (at < 0) return true;
         used[at] = true;
-        if (s[at] < end) return false;
+        if (s[at] < end || s[at] > ((int64_t)1 << 44) / (n[at] - 1)) return false;      // (no memory is that large)
         end = s[at] * (n[at] - 1) + end;
     }
     return true;

@@ -588,7 +588,7 @@ static int check_strides(int64_t B, int64_t H, int64_t n, int64_t sb, int64_t sh
             if (!used[i] && e[i] > 1 && (at < 0 || s[i] < s[at])) at = i;
         if (at < 0) break;
         used[at] = true;
-        if (s[at] < end || s[at] >= (int64_t)1 << 39) return PSK_ERR_SHAPE;
+        if (s[at] < end || s[at] >= (int64_t)1 << 39 || s[at] > ((int64_t)1 << 44) / (e[at] - 1)) return PSK_ERR_SHAPE;      // (no memory is that large)
         if (s[at] * esz % 16) return PSK_ERR_ALIGN;
         end += s[at] * (e[at] - 1);
     }

@@ -39,7 +39,7 @@ def window_calls(L, s):
 
 @pytest.mark.parametrize("field,value,code", [
     ("dtype", 2, -1), ("eps", -1e-9, -1), ("eps", float("nan"), -1), ("eps", float("inf"), -1), ("n0", 0, -3), ("n1", -2, -3), ("n2", 0, -3), ("cols", 0, -3),
-    ("cols", 8193, -2), ("n0", 1 << 30, -3), ("zs", (64 * 12, 32, 64 * 12 * 4), -3), ("zs", (0, 64, 64 * 12 * 4), -3)])
+    ("cols", 8193, -2), ("n0", 1 << 30, -3), ("zs", (64 * 12, 32, 64 * 12 * 4), -3), ("zs", (0, 64, 64 * 12 * 4), -3), ("zs", (1 << 62, 64, 64 * 12 * 4), -3), ("zs", (64 * 12, 64, 1 << 43), -3)])
 def test_layer_norm(L, field, value, code):
     s = norm()
     setattr(s, field, (c_int64 * 3)(*value) if isinstance(value, tuple) else value)
@@ -73,7 +73,7 @@ def test_window(L, field, value, code):
 
 @pytest.mark.parametrize("fields,code", [
     (dict(n=0), -3), (dict(n=1 << 29), -3), (dict(q_stride_n=32), -3), (dict(q_stride_h=0), -3), (dict(kv_stride_b=6400), -3), (dict(q_stride_n=68, q_stride_h=6800, q_stride_b=27200), -4),
-    (dict(kv_stride_h=6401, kv_stride_b=2 * 6401), -4), (dict(path=2, dtype=0), -2)])
+    (dict(kv_stride_h=6401, kv_stride_b=2 * 6401), -4), (dict(q_stride_n=1 << 38), -3), (dict(path=2, dtype=0), -2)])
 def test_window_rows(L, fields, code):
     s = window()
     for f, v in fields.items():
