@@ -300,7 +300,8 @@ int psk_layer_norm_bwd(const psk_norm_shape* shape, const void* X, const float* 
  *   lse            DEVICE [B, H, n] fp32, written by the forward, read by the backward
  *   lengths        DEVICE [B] int32 or NULL (all n); clamped to 0 .. n
  *   workspace      DEVICE scratch, 256-byte aligned, >= psk_window_workspace_bytes(shape, for_backward) (0 for a bad
- *                  shape); its first word is the status that psk_check() reads
+ *                  shape); its first word is the status that psk_check() reads.  One call's at a time: calls, and replays
+ *                  of captured ones, that may run side by side take one each (as for psk_layer_norm_bwd)
  * Query head h reads key head h / (H / Hkv); dK and dV are summed over the query heads that share one, in a fixed
  * order.  h = 64, any n >= 1, window >= 1, sinks >= 0, scale > 0.  fp32 storage: CUDA cores, fp32 arithmetic.  bf16 storage: tensor
  * cores with fp32 accumulation, weights and their gradients rounded to bf16 once as operands (PSK_PATH_CUDA_CORES: fp32
