@@ -273,7 +273,8 @@ int psk_decode_step(const psk_shape* shape, const void* q, const void* k, const 
  *   dgain, dbias  DEVICE fp32 [cols] or NULL, overwritten; sums in a fixed order: the same bits every time
  *   workspace     DEVICE scratch for the backward, 16-byte aligned, >= psk_layer_norm_workspace_bytes(shape)
  *                 (0 for a bad shape); not read if dgain and dbias are NULL
- * cols from 1 to 8192, fewer than 2^31 rows.  fp32 arithmetic.  No alignment is asked for: rows that do not lie on 16 bytes
+ * cols from 1 to 8192, fewer than 2^31 rows.  fp32 arithmetic: the sum of a row's squared deviations has to fit fp32, as for spreads (standard
+ * deviations) up to 1e17; with eps = 0 also from 1e-17 on.  No alignment is asked for: rows that do not lie on 16 bytes
  * are read by two values or by one. */
 typedef struct {
     int32_t n0, n1, n2, cols;

@@ -317,8 +317,9 @@ norm_bwd_kernel(const __grid_constant__ NormArgs a) {
         for (int i = 0; i < 3; ++i) t[i] = vsum(t2[i]);
         row_sums<G>(t, red2);
         const float rstd = rsqrtf(fmaf(t[0], a.over_cols, a.eps));
-        // dx = rstd g - rstd sum(g) / C - dev rstd^3 sum(g dev) / C
-        const float k1 = -rstd * t[1] * a.over_cols, k2 = -rstd * rstd * rstd * (t[2] * a.over_cols);
+        // dx = rstd g - rstd sum(g) / C - xhat rstd (rstd sum(g dev) / C), xhat = dev rstd.  (In this order: for spreads beyond 1e13 or
+        // below 1e-13 the cube of rstd is not a normal number any more, while xhat and its product with g are near one.)
+        const float k1 = -rstd * t[1] * a.over_cols, k2 = -rstd * (rstd * (t[2] * a.over_cols));
         W rstd2, k12, k22;
         vset(rstd2, rstd);
         vset(k12, k1);
@@ -335,10 +336,10 @@ norm_bwd_kernel(const __grid_constant__ NormArgs a) {
                 gained(g, d, k);
 #pragma unroll
                 for (int i = 0; i < P; ++i) {
-                    const W dev = vadd(f[i], mean2);
-                    dg[k * P + i] = vfma(vmul(d[i], rstd2), dev, dg[k * P + i]);
+                    const W xhat = vmul(vadd(f[i], mean2), rstd2);
+                    dg[k * P + i] = vfma(d[i], xhat, dg[k * P + i]);
                     db[k * P + i] = vadd(db[k * P + i], d[i]);
-                    f[i] = vfma(dev, k22, vfma(g[i], rstd2, k12));
+                    f[i] = vfma(xhat, k22, vfma(g[i], rstd2, k12));
                 }
                 Pack<T, V>::store(row + vec * V, f);
             }

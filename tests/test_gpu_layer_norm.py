@@ -247,3 +247,37 @@ def test_refusals():
         with pytest.raises(psk.PskError) as e:
             psk.layer_norm_fwd(**bad)
         assert e.value.code == code
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("cols", [64, 65, 66, 768, 4096])
+@pytest.mark.parametrize("spread,eps", [(1e15, 1e-6), (1e17, 1e-6), (1e-14, 0.0), (1e-17, 0.0)])
+def test_spreads_far_from_one(dtype, cols, spread, eps):
+    """rstd cubed is beyond fp32 for these rows; every factor of the formulas, and their products in a fitting order, are not."""
+    X, dY = rows_of(dtype, 50, cols, seed=cols + 2), rows_of(dtype, 50, cols, seed=cols + 3)
+    X = (X.float() * spread).to(X.dtype)
+    # gradients with a part along the rows, so that the projection's term is as large as the others
+    dY = (dY.float() + X.float() / X.float().std(-1, unbiased=False, keepdim=True)).to(X.dtype)
+    gain, bias = 1 + 0.1 * rows_of("f32", cols, seed=3), rows_of("f32", cols, seed=4)
+    Y = psk.layer_norm_fwd(X, gain, bias, eps)
+    dX, dgain, dbias = psk.layer_norm_bwd(X, gain, dY, eps)
+    check(dtype, X, gain, bias, dY, Y, dX, dgain, dbias, eps)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("cols", [64, 70, 77])
+def test_an_output_of_other_strides(dtype, cols):
+    """Rows are worked on in the order of X's strides; an output laid out in another order gets each row in its place."""
+    B, n, H = 3, 45, 5
+    X, dY = rows_of(dtype, B, H, n, cols, seed=31), rows_of(dtype, B, H, n, cols, seed=32)
+    gain = 1 + 0.1 * rows_of("f32", cols, seed=33)
+    dense, (dXd, dgd, dbd) = psk.layer_norm_fwd(X, gain), psk.layer_norm_bwd(X, gain, dY)
+    for order in ((0, 2, 1), (1, 0, 2), (2, 1, 0), (2, 0, 1)):
+        shape, back = [(B, H, n)[i] for i in order], [order.index(i) for i in range(3)]
+        into, dinto = (torch.empty(*shape, cols, dtype=X.dtype, device="cuda").permute(*back, 3) for _ in range(2))
+        got = psk.layer_norm_fwd(X, gain, out=into)
+        assert got is into
+        assert torch.equal(into, dense)
+        dX, dgain, dbias = psk.layer_norm_bwd(X, gain, dY, out=dinto)
+        assert dX is dinto or dX.data_ptr() == dinto.data_ptr()
+        assert torch.equal(dinto, dXd) and torch.equal(dgain, dgd) and torch.equal(dbias, dbd)
