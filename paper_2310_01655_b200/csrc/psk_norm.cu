@@ -137,10 +137,11 @@ __device__ __forceinline__ float over_cols(const NormArgs& a, float s) {
 }
 
 // A row's lanes, and what they hold: accesses l, l + G, ... of V values each, as kPer words each.
-template <int V, int NV, int G> struct RowMap {
+template <typename T, int V, int NV, int G> struct RowMap {
     static constexpr int kRowsPerCta = kNormThreads / G, kPer = (V + 1) / 2, kPairs = kPer * NV, kValues = V * NV;
-    // rows in flight per lane, as registers allow
-    static constexpr int kFwdRows = kValues <= 8 ? 4 : (kValues <= 16 ? 4 : 3), kBwdRows = kValues <= (V == 1 ? 8 : 16) ? 2 : 1;
+    // rows in flight per lane, as registers allow.  Backward: beside two sums (and the gain) of every column, two rows of x and dy fit 128 registers
+    // up to 8 values a lane, and up to 16 where these are bf16 in pairs (16 384 rows in fp32, us with two / one: 4096 columns 243 / 174, 3002 236 / 172).
+    static constexpr int kFwdRows = kValues <= 16 ? 4 : 3, kBwdRows = kValues <= (sizeof(T) == 2 && V > 1 ? 16 : 8) ? 2 : 1;
 };
 // a parameter's values at the lane's columns (1 or 0 where there is none)
 template <int V> __device__ __forceinline__ void load_param(typename Word<V>::type* f, const float* p, int vec, bool in, float none) {
@@ -163,7 +164,7 @@ __device__ __forceinline__ void load_row(Pack<T, V> (&x)[NV], const NormArgs& a,
 template <typename T, int V, int NV, int G>
 __global__ void __launch_bounds__(kNormThreads)
 norm_fwd_kernel(const __grid_constant__ NormArgs a) {
-    using M = RowMap<V, NV, G>;
+    using M = RowMap<T, V, NV, G>;
     typedef typename Word<V>::type W;
     constexpr int P = M::kPer, D = M::kFwdRows;
     constexpr bool kKeep = M::kValues <= 24;              // gain and bias in registers, or read again for every row (from L1)
@@ -236,12 +237,14 @@ norm_fwd_kernel(const __grid_constant__ NormArgs a) {
 }
 
 template <typename T, int V, int NV, int G>
-__global__ void __launch_bounds__(kNormThreads, RowMap<V, NV, G>::kValues <= 16 ? 2 : 1)
+__global__ void __launch_bounds__(kNormThreads, RowMap<T, V, NV, G>::kValues <= 16 ? 2 : 1)
 norm_bwd_kernel(const __grid_constant__ NormArgs a) {
-    using M = RowMap<V, NV, G>;
+    using M = RowMap<T, V, NV, G>;
     typedef typename Word<V>::type W;
     constexpr int P = M::kPer, D = M::kBwdRows;
-    constexpr bool kKeep = M::kValues <= 16;
+    // the gain in registers, or read again for every row (from L1): where that takes wide accesses and they are short (4096 columns in fp32 174 / 160,
+    // 3002, by twos, 172 / 202)
+    constexpr bool kKeep = M::kValues <= (sizeof(T) == 4 && V == 4 ? 8 : 16);
     __shared__ float red1[1][kNormWarps], red2[3][kNormWarps];
     extern __shared__ float sums[];                                       // [2][cols]
     pdl_sync();
@@ -336,8 +339,9 @@ norm_bwd_kernel(const __grid_constant__ NormArgs a) {
                 gained(g, d, k);
 #pragma unroll
                 for (int i = 0; i < P; ++i) {
-                    const W xhat = vmul(vadd(f[i], mean2), rstd2);
-                    dg[k * P + i] = vfma(d[i], xhat, dg[k * P + i]);
+                    const W dev = vadd(f[i], mean2), xhat = vmul(dev, rstd2);
+                    // (by twos, 16 values or more, xhat does not fit the registers as well: 16 384 rows of 3002 in bf16, 97 us so, 136 as the others; rows of 1002 136, 131)
+                    dg[k * P + i] = V == 2 && M::kValues > 8 ? vfma(vmul(d[i], rstd2), dev, dg[k * P + i]) : vfma(d[i], xhat, dg[k * P + i]);
                     db[k * P + i] = vadd(db[k * P + i], d[i]);
                     f[i] = vfma(xhat, k22, vfma(g[i], rstd2, k12));
                 }
@@ -454,7 +458,7 @@ int check_shape(const psk_norm_shape* sh, bool backward) {
 
 template <typename T, int V, int NV, int G>
 cudaError_t launch(const NormArgs& a, bool backward, cudaStream_t s) {
-    using M = RowMap<V, NV, G>;
+    using M = RowMap<T, V, NV, G>;
     const uint64_t want = ((uint64_t)a.rows + M::kRowsPerCta - 1) / M::kRowsPerCta;
     const int grid = (int)(want < (uint64_t)kNormMaxCtas ? want : (uint64_t)kNormMaxCtas);
     if (!backward) {
