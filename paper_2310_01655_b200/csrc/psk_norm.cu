@@ -456,17 +456,22 @@ int check_shape(const psk_norm_shape* sh, bool backward) {
     return rows_apart(n, backward ? sh->zs : sh->ys, sh->cols) ? PSK_OK : PSK_ERR_SHAPE;
 }
 
+template <typename M>
+int grid_of(const NormArgs& a) {
+    const uint64_t want = ((uint64_t)a.rows + M::kRowsPerCta - 1) / M::kRowsPerCta;
+    return (int)(want < (uint64_t)kNormMaxCtas ? want : (uint64_t)kNormMaxCtas);
+}
+template <typename T, int V, int NV, int G>
+cudaError_t launch_fwd(const NormArgs& a, cudaStream_t s) {
+    prof_begin("norm_fwd_kernel", s);
+    launch_pdl(norm_fwd_kernel<T, V, NV, G>, dim3(grid_of<RowMap<T, V, NV, G>>(a)), dim3(kNormThreads), 0, s, a);
+    prof_end(s);
+    return cudaGetLastError();
+}
 template <typename T, int V, int NV, int G>
 cudaError_t launch(const NormArgs& a, bool backward, cudaStream_t s) {
-    using M = RowMap<T, V, NV, G>;
-    const uint64_t want = ((uint64_t)a.rows + M::kRowsPerCta - 1) / M::kRowsPerCta;
-    const int grid = (int)(want < (uint64_t)kNormMaxCtas ? want : (uint64_t)kNormMaxCtas);
-    if (!backward) {
-        prof_begin("norm_fwd_kernel", s);
-        launch_pdl(norm_fwd_kernel<T, V, NV, G>, dim3(grid), dim3(kNormThreads), 0, s, a);
-        prof_end(s);
-        return cudaGetLastError();
-    }
+    if (!backward) return launch_fwd<T, V, NV, G>(a, s);
+    const int grid = grid_of<RowMap<T, V, NV, G>>(a);
     const bool params = a.dgain != nullptr || a.dbias != nullptr;
     const size_t smem = params ? 2 * (size_t)a.cols * sizeof(float) : 0;
     cudaError_t e = cudaFuncSetAttribute(norm_bwd_kernel<T, V, NV, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * kNormMaxCols * (int)sizeof(float));
@@ -510,7 +515,7 @@ cudaError_t dispatch(const NormArgs& a, int width, bool backward, cudaStream_t s
     if (nvec <= 32) return launch<T, V, 2, 16>(a, backward, s);
     if (nvec <= 64) return launch<T, V, 2, 32>(a, backward, s);
     // (the forward has the registers for more values in a lane; 65 536 rows of 768, us with 32 / 64 lanes to a row: forward 44 / 57, backward 179 / 85)
-    if (!backward && nvec <= 96) return launch<T, V, 3, 32>(a, backward, s);
+    if (!backward && nvec <= 96) return launch_fwd<T, V, 3, 32>(a, s);
     if (nvec <= 128) return launch<T, V, 2, 64>(a, backward, s);
     if (nvec <= 256) return launch<T, V, 2, 128>(a, backward, s);
     if (nvec <= 512) return launch<T, V, 2, 256>(a, backward, s);
