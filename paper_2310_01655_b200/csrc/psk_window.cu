@@ -634,6 +634,12 @@ WinArgs key_side(const WinArgs& a, int tile) {
 // Bytes of the sums over query heads and over parts.
 static size_t row_sum_bytes(const WinArgs& k) { return k.hs > 1 ? (size_t)k.B * k.Hkv * k.n * 2 * 64 * sizeof(float) : 0; }
 static size_t partial_bytes(const WinArgs& k) { return k.parts > 0 ? (size_t)k.B * k.Hkv * (k.parts + 1) * 2 * k.sinks * 64 * sizeof(float) : 0; }
+// Bytes of the lists of rows that the tensor-core kernels form again (psk_window_tc.cu); k: null for the forward.
+static size_t redo_bytes(const WinArgs& a, const WinArgs* k) {
+    // (the forward's 8 entries an item, the query side's 4; one workspace may serve both calls)
+    const size_t tiles = ((size_t)a.n + 127) / 128, rows = tiles * a.B * a.H, keys = k == nullptr ? 0 : (tiles + k->parts) * k->B * k->Hkv;
+    return (rows > keys ? rows : keys) * 8 * sizeof(uint2);
+}
 static bool on_tensor_cores(const psk_window_shape* sh) { return sh->dtype == PSK_BF16 && sh->path != PSK_PATH_CUDA_CORES; }
 // Device waits are bounded by a second, and some last as long as a tile: 2^25 rows of query heads on one tile of keys take the key side 0.4 s.
 static int check_attention(const psk_window_shape* sh) {
@@ -664,12 +670,12 @@ extern "C" {
 
 size_t psk_window_workspace_bytes(const psk_window_shape* shape, int for_backward) {
     if (check_attention(shape) != PSK_OK) return 0;
-    if (!for_backward) return kStatusBytes;
     const WinArgs a = args_of(shape);
+    if (!for_backward) return kStatusBytes + (shape->dtype == PSK_BF16 ? align_up(redo_bytes(a, nullptr)) : 0);
     size_t sums = 0;                                      // (enough for either path)
     for (int tile = kTile; tile <= 128; tile += 64) {
         const WinArgs k = key_side(a, tile);
-        const size_t bytes = align_up(row_sum_bytes(k)) + align_up(partial_bytes(k));
+        const size_t bytes = align_up(row_sum_bytes(k)) + align_up(partial_bytes(k)) + (tile == 128 && shape->dtype == PSK_BF16 ? align_up(redo_bytes(a, &k)) : 0);
         if (bytes > sums) sums = bytes;
     }
     return kStatusBytes + 2 * align_up((size_t)a.B * a.H * a.n * sizeof(float)) + sums;
@@ -688,6 +694,7 @@ int psk_window_attn_fwd(const psk_window_shape* shape, const void* Q, const void
     WinArgs a = args_of(shape);
     a.Q = Q; a.K = K; a.V = V; a.out = O; a.lse = lse; a.lengths = lengths;
     int* status = static_cast<int*>(workspace);
+    a.redo = reinterpret_cast<uint2*>(static_cast<char*>(workspace) + kStatusBytes);
     cudaError_t e;
     if (on_tensor_cores(shape)) {
         e = tc_window_fwd(a, status, s);
@@ -715,6 +722,8 @@ int psk_window_attn_bwd(const psk_window_shape* shape, const void* Q, const void
     WinArgs k = key_side(a, on_tensor_cores(shape) ? 128 : kTile);
     k.rows = a.stat_d + align_up((size_t)a.B * a.H * a.n * sizeof(float)) / sizeof(float);
     k.partial = k.rows + align_up(row_sum_bytes(k)) / sizeof(float);
+    // (first the query side's, then the key side's)
+    a.redo = k.redo = reinterpret_cast<uint2*>(k.partial + align_up(partial_bytes(k)) / sizeof(float));
     int* status = static_cast<int*>(workspace);
     cudaError_t e;
     if (on_tensor_cores(shape)) {

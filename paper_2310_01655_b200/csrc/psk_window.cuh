@@ -32,6 +32,8 @@ struct WinArgs {
     // if they were key heads of their own (Hkv and G there: times and through hs); their sums are added up from `rows` [B Hkv][dK, dV][n][64].
     int hs;
     float* rows;
+    // Tensor-core kernels: rows that are formed again when a CTA has done all else, [item](x [2], key side)[warps of its rows] (redo_* below)
+    uint2* redo;
 };
 __device__ __forceinline__ float* sum_row(const WinArgs& a, int b, int hk, int which, int j) {
     return a.rows + ((((int64_t)b * a.Hkv + hk) * 2 + which) * a.n + j) * 64;
@@ -64,7 +66,8 @@ __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0
 // stands there, it comes through as NaN.  So a result row that is not finite, though its own statistics are no NaN, and that shares a tile with
 // such a row that it does not see (*_tainted) is formed again here from the pairs that count alone (lane l holds columns 2 l and
 // 2 l + 1).  Slow, and only there: eight pairs on their way at a time, and no further than to the pair that makes all of
-// the row NaN.  (The other warps wait for this one, with a limit of a second.)
+// the row NaN.  In the tensor-core kernels waits have a limit of a second, and a row over a long sequence takes a warp longer: there such rows
+// are only noted, and looked at when nobody in the CTA waits any more.
 constexpr int kRedo = 8;
 template <typename T> __device__ __forceinline__ float2 ld2(const T* p) { return make_float2(ldf(p), ldf(p + 1)); }
 template <typename T> __device__ __forceinline__ void st2(T* p, float2 v) { stf(p, v.x); stf(p + 1, v.y); }

@@ -139,10 +139,23 @@ __device__ __forceinline__ void store_partial(float* dst, uint32_t taddr, float 
             if (live) *reinterpret_cast<float4*>(dst + q + j) = make_float4(o[j] * f, o[j + 1] * f, o[j + 2] * f, o[j + 3] * f);
     }
 }
-// two values of a staged row, by each lane of a warp (whose columns lie in that half)
-__device__ __forceinline__ void stage_pair(uint8_t* st, int row, float2 v, int half = -1) {
-    const int lane = threadIdx.x % 32;
-    if (half < 0 || lane / 16 == half) *reinterpret_cast<uint32_t*>(st + swz128_offset(row, lane / 4) + lane % 4 * 4) = pack_bf16(v.x, v.y);
+
+// Rows to be formed again (psk_window.cuh): a warp's list of items, through memory.  An entry: which of the warp's 32 rows, and the code of the
+// item noted before it.
+constexpr uint32_t kNoItem = 0xffffffffu;
+__device__ __forceinline__ void redo_note(uint2* entry, uint32_t code, unsigned rows, uint32_t& last) {
+    if (rows != 0 && threadIdx.x % 32 == 0) { *entry = make_uint2(rows, last); last = code; }
+}
+// f(code, row) for each, by the whole warp, when the CTA's tiles have arrived in memory
+template <typename Entry, typename F>
+__device__ __forceinline__ void redo_noted(uint32_t last, const Entry& entry, const F& f) {
+#pragma unroll 1
+    for (uint32_t code = last; code != kNoItem;) {
+        const uint2 e = *entry(code);
+#pragma unroll 1
+        for (unsigned rows = e.x; rows != 0; rows &= rows - 1) f(code, __ffs(rows) - 1);
+        code = e.y;
+    }
 }
 
 // The rows r0, r0 + 1, ... below `end` and zeros behind them as a TMA load would leave them, by a whole warp.  For the tile in which
@@ -213,6 +226,8 @@ tc_win_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
     uint8_t* smem = align1024(smem_raw);
     __shared__ __align__(16) Sched sched;
     __shared__ float s_top[2][kRows], s_sum[2][kRows];
+    __shared__ unsigned s_bad[2][4];                      // a row's halves that are not finite, by warps
+    __shared__ uint32_t s_redo[8];
     __shared__ uint64_t bar_q[2], free_q[2], bar_k[2], free_k[2], bar_v[2], free_v[2], bar_s, bar_read, bar_p, bar_o;
     __shared__ uint32_t tm_slot;
     const int tid = threadIdx.x, warp = warp_index();
@@ -225,6 +240,7 @@ tc_win_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
         mbar_init(&bar_s, 1); mbar_init(&bar_read, 8); mbar_init(&bar_p, 8); mbar_init(&bar_o, 1);
         mbar_fence_init();
     }
+    if (tid < 8) s_redo[tid] = kNoItem;
     pdl_sync();
     if (blockIdx.x == 0 && tid == 0) *status = 0;
     if (warp == Fwd::kMma) { tmem_alloc(&tm_slot, Fwd::kTmem); tmem_relinquish(); }
@@ -432,16 +448,12 @@ tc_win_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
                 const bool fine = stage_half(st, row, half, lane_tm + Fwd::cO, 1.f / l, live) || !finite(v);      // (where v is not, the row is NaN)
                 tc_fence_before();
                 if (ok && half == 0 && i < a.n) lse[i] = live ? v : neg_inf();
-                unsigned bad = __ballot_sync(0xffffffffu, ok && !fine && live);
-                while (bad != 0) {
-                    const int k = __ffs(bad) - 1, r = i_first + k, hk = p.h / a.G;
-                    bad &= bad - 1;
-                    const bf16 *K = (const bf16*)a.K + p.b * a.kb + hk * a.kh, *V = (const bf16*)a.V + p.b * a.kb + hk * a.kh;
-                    if (row_tainted(K, V, a.kn, r, a.window, a.sinks, p.len))
-                        stage_pair(st, warp % 4 * 32 + k, redo_out_row((const bf16*)a.Q + p.b * a.qb + p.h * a.qh + (int64_t)r * a.qn, K, V, a.kn, r, a.window, a.sinks, c), half);
-                }
+                const unsigned bad = __ballot_sync(0xffffffffu, ok && !fine && live);
+                if (lane == 0) s_bad[half][warp % 4] = bad;
                 fence_proxy_async_smem();
                 bar_sync(5, Fwd::kRowThreads);
+                // (each of a row's two warps takes every other one)
+                redo_note(a.redo + (size_t)index * 8 + warp, index, (s_bad[0][warp % 4] | s_bad[1][warp % 4]) & (half ? 0xaaaaaaaau : 0x55555555u), s_redo[warp]);
                 if (tid == 0 && !cta_gave_up()) { tma_store_4d(&mapO, st, 0, p.row0, p.h, p.b); bulk_commit(); }
                 stored = true;
             } else {                                      // behind the sequence's end
@@ -452,11 +464,20 @@ tc_win_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
             if (bar_any(5, Fwd::kRowThreads, index < 0)) index = -1;        // (all of them or none: they share barriers)
             if (lane == 0) sched_taken(sched, it);
         }
-        if (tid == 0) bulk_wait_read();
+        if (tid == 0) bulk_wait_all();
     }
     tc_fence_before();
     __syncthreads();
     if (warp == Fwd::kMma) { cta_teardown_warp(); tmem_dealloc(tm, Fwd::kTmem); }
+    if (warp < 8 && !cta_gave_up())
+        redo_noted(s_redo[warp], [&](uint32_t code) { return a.redo + (size_t)code * 8 + warp; }, [&](uint32_t code, int k) {
+            const Item p = item_of(a, map, code);
+            const int r = p.row0 + warp % 4 * 32 + k, hk = p.h / a.G;
+            const bf16 *K = (const bf16*)a.K + p.b * a.kb + hk * a.kh, *V = (const bf16*)a.V + p.b * a.kb + hk * a.kh;
+            const int64_t at = p.b * a.qb + p.h * a.qh + r * a.qn;
+            if (row_tainted(K, V, a.kn, r, a.window, a.sinks, p.len))
+                st2((bf16*)a.out + at + 2 * (tid % 32), redo_out_row((const bf16*)a.Q + at, K, V, a.kn, r, a.window, a.sinks, a.c));
+        });
 }
 
 // ---------------------------------------------------------------------------
@@ -501,6 +522,7 @@ tc_win_dq_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
     uint8_t* smem = align1024(smem_raw);
     __shared__ __align__(16) Sched sched;
     __shared__ float s_lse[2][kRows];
+    __shared__ uint32_t s_redo[4 * kGroups];
     __shared__ uint64_t bar_q[2], free_q[2], bar_kv[Dq::kStages], free_kv[Dq::kStages], bar_s[kGroups], bar_ds[kGroups], bar_fin[4], bar_acc;
     __shared__ uint32_t tm_slot;
     const int tid = threadIdx.x, warp = warp_index(), lane = tid % 32;
@@ -514,6 +536,7 @@ tc_win_dq_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
         mbar_init(&bar_acc, 4);
         mbar_fence_init();
     }
+    if (tid < 4 * kGroups) s_redo[tid] = kNoItem;
     pdl_sync();
     if (blockIdx.x == 0 && tid == 0) *status = 0;
     if (warp == Dq::kMma) { tmem_alloc(&tm_slot, Dq::kTmem); tmem_relinquish(); }
@@ -716,17 +739,9 @@ tc_win_dq_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
                     bar_sync(1 + group, kRows);
                     const bool live = i < p.len, fine = stage_row(st, row, lane_tm + Dq::cDq, a.scale, live);
                     tc_fence_before();
-                    unsigned bad = __ballot_sync(0xffffffffu, ok && !fine && live && stat.x == stat.x && stat.y == stat.y);      // (with a NaN there the row is NaN)
+                    const unsigned bad = __ballot_sync(0xffffffffu, ok && !fine && live && stat.x == stat.x && stat.y == stat.y);      // (with a NaN there the row is NaN)
                     if (lane == 0) mbar_arrive(&bar_acc);
-                    while (bad != 0) {
-                        const int k = __ffs(bad) - 1, r = i_first + k, hk = p.h / a.G;
-                        bad &= bad - 1;
-                        const int64_t at = qoff + (int64_t)r * a.qn;
-                        const bf16 *K = (const bf16*)a.K + p.b * a.kb + hk * a.kh, *V = (const bf16*)a.V + p.b * a.kb + hk * a.kh;
-                        const float2 sr = make_float2(-__shfl_sync(0xffffffffu, stat.x, k), -__shfl_sync(0xffffffffu, stat.y, k));
-                        if (row_tainted(K, V, a.kn, r, a.window, a.sinks, p.len))
-                            stage_pair(st, warp % 4 * 32 + k, redo_dq_row((const bf16*)a.Q + at, (const bf16*)a.dO + at, K, V, a.kn, r, a.window, a.sinks, a.c, a.scale, sr));
-                    }
+                    redo_note(a.redo + (size_t)index * 4 + warp % 4, index, bad, s_redo[warp]);
                     fence_proxy_async_smem();
                     bar_sync(1 + group, kRows);
                     if (row == 0 && !cta_gave_up()) { tma_store_4d(&mapDq, st, 0, p.row0, p.h, p.b); bulk_commit(); }
@@ -740,11 +755,21 @@ tc_win_dq_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
             if (bar_any(1 + group, kRows, index < 0)) index = -1;            // (a whole warpgroup or none of it: it shares barriers)
             if (lane == 0) sched_taken(sched, it);
         }
-        if (row == 0) bulk_wait_read();
+        if (row == 0) bulk_wait_all();
     }
     tc_fence_before();
     __syncthreads();
     if (warp == Dq::kMma) { cta_teardown_warp(); tmem_dealloc(tm, Dq::kTmem); }
+    if (warp < 4 * kGroups && !cta_gave_up())
+        redo_noted(s_redo[warp], [&](uint32_t code) { return a.redo + (size_t)code * 4 + warp % 4; }, [&](uint32_t code, int k) {
+            const Item p = item_of(a, map, code);
+            const int r = p.row0 + warp % 4 * 32 + k, hk = p.h / a.G;
+            const bf16 *K = (const bf16*)a.K + p.b * a.kb + hk * a.kh, *V = (const bf16*)a.V + p.b * a.kb + hk * a.kh;
+            const int64_t at = p.b * a.qb + p.h * a.qh + r * a.qn, stat = ((int64_t)p.b * a.H + p.h) * a.n + r;
+            if (row_tainted(K, V, a.kn, r, a.window, a.sinks, p.len))
+                st2((bf16*)a.dQ + at + 2 * lane, redo_dq_row((const bf16*)a.Q + at, (const bf16*)a.dO + at, K, V, a.kn, r, a.window, a.sinks, a.c, a.scale,
+                                                            make_float2(-a.stat_l[stat], -a.stat_d[stat])));
+        });
 }
 
 // ---------------------------------------------------------------------------
@@ -767,6 +792,7 @@ tc_win_dkv_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constan
     uint8_t* smem = align1024(smem_raw);
     __shared__ __align__(16) Sched sched;
     __shared__ __align__(16) float s_stat[Dkv::kStages][2][64];          // -lse log2(e), -D
+    __shared__ uint32_t s_redo[4 * kGroups];
     __shared__ uint64_t bar_kv[2], free_kv[2], bar_qg[Dkv::kStages], free_qg[Dkv::kStages], bar_s[kGroups], bar_ds[kGroups], bar_fin[4], bar_acc;
     __shared__ uint32_t tm_slot;
     const int tid = threadIdx.x, warp = warp_index(), lane = tid % 32;
@@ -780,6 +806,7 @@ tc_win_dkv_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constan
         mbar_init(&bar_acc, 8);
         mbar_fence_init();
     }
+    if (tid < 4 * kGroups) s_redo[tid] = kNoItem;
     pdl_sync();
     if (warp == Dkv::kMma) { tmem_alloc(&tm_slot, Dkv::kTmem); tmem_relinquish(); }
     tc_fence_before();
@@ -796,6 +823,11 @@ tc_win_dkv_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constan
         }
     };
     auto tiles_of = [&](const KeyItem& p) { return (p.end(a, kRows) - p.begin + 63) / 64; };       // steps per query head
+    // where a row's gradients (0: dK, 1: dV) are added up from
+    auto sum_place = [&](const KeyItem& p, int which, int r) -> float* {
+        if (p.part >= 0 && r < a.sinks) return partial_row(a, p.b, p.h, p.part, which, r);
+        return p.part <= 0 && a.hs > 1 ? sum_row(a, p.b, p.h, which, p.key0 + r) : nullptr;
+    };
     if (warp == Dkv::kLoad) {
         bool ok = true;
         int t = 0, items = 0;
@@ -970,15 +1002,10 @@ tc_win_dkv_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constan
                     tc_fence_after();
                     bar_sync(1 + group, kRows);
                     const bool live = j < p.len;
-                    // where this row's gradients are added up from
-                    auto sum_place = [&](int r) -> float* {
-                        if (p.part >= 0 && r < a.sinks) return partial_row(a, p.b, p.h, p.part, has_k ? 0 : 1, r);
-                        return p.part <= 0 && a.hs > 1 ? sum_row(a, p.b, p.h, has_k ? 0 : 1, p.key0 + r) : nullptr;
-                    };
                     const uint32_t from = lane_tm + (has_k ? Dkv::cDk : Dkv::cDv);
                     const float f = has_k ? a.scale : 1.f;
                     if (PARTS) {
-                        float* to = live && ok ? sum_place(row) : nullptr;
+                        float* to = live && ok ? sum_place(p, has_k ? 0 : 1, row) : nullptr;
                         if (__any_sync(0xffffffffu, to != nullptr)) store_partial(to, from, f, to != nullptr);
                     }
                     if (PARTS && p.part > 0) {
@@ -987,18 +1014,10 @@ tc_win_dkv_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constan
                     } else {
                         const bool fine = stage_row(st, row, from, f, live);
                         tc_fence_before();
-                        unsigned bad = __ballot_sync(0xffffffffu, ok && !fine && live);
+                        const unsigned bad = __ballot_sync(0xffffffffu, ok && !fine && live);
                         if (lane == 0) mbar_arrive(&bar_acc);
-                        if (PARTS) __syncwarp();          // (the partial row is written over below)
-                        while (bad != 0) {
-                            const int k = __ffs(bad) - 1, r = warp % 4 * 32 + k;
-                            bad &= bad - 1;
-                            const bool part = PARTS && p.part == 0 && r < a.sinks;
-                            if (!key_tainted<bf16>(a, p.b, p.h, j_first + k, p.len, p.stop)) continue;
-                            const KeyRow key = redo_dkv_row<bf16>(a, p.b, p.h, j_first + k, p.len, part ? p.stop : p.len);
-                            stage_pair(st, r, has_k ? key.dk : key.dv);
-                            if (PARTS && sum_place(r) != nullptr) st2(sum_place(r) + 2 * lane, has_k ? key.dk : key.dv);
-                        }
+                        const uint32_t code = 2 * (uint32_t)index + (has_k ? 0 : 1);
+                        redo_note(a.redo + (size_t)code * 4 + warp % 4, code, bad, s_redo[warp]);
                         fence_proxy_async_smem();
                         bar_sync(1 + group, kRows);
                         if (row == 0 && !cta_gave_up() && (!PARTS || a.hs == 1)) { tma_store_4d(has_k ? &mapDk : &mapDv, st, 0, p.key0, p.h, p.b); bulk_commit(); }
@@ -1013,11 +1032,22 @@ tc_win_dkv_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constan
             if (bar_any(1 + group, kRows, index < 0)) index = -1;            // (a whole warpgroup or none of it: it shares barriers)
             if (lane == 0) sched_taken(sched, it);
         }
-        if (row == 0) bulk_wait_read();
+        if (row == 0) bulk_wait_all();
     }
     tc_fence_before();
     __syncthreads();
     if (warp == Dkv::kMma) { cta_teardown_warp(); tmem_dealloc(tm, Dkv::kTmem); }
+    if (warp < 4 * kGroups && !cta_gave_up())
+        redo_noted(s_redo[warp], [&](uint32_t code) { return a.redo + (size_t)code * 4 + warp % 4; }, [&](uint32_t code, int k) {
+            const KeyItem p = item((int)(code / 2));
+            const int which = (int)(code % 2), r = warp % 4 * 32 + k, j = p.key0 + r;
+            if (!key_tainted<bf16>(a, p.b, p.h, j, p.len, p.stop)) return;
+            const KeyRow key = redo_dkv_row<bf16>(a, p.b, p.h, j, p.len, PARTS && p.part == 0 && r < a.sinks ? p.stop : p.len);
+            const float2 v = which ? key.dv : key.dk;
+            float* sum = PARTS ? sum_place(p, which, r) : nullptr;
+            if (sum != nullptr) st2(sum + 2 * lane, v);
+            else st2((bf16*)(which ? a.dV : a.dK) + p.b * a.kb + (PARTS ? p.h / a.hs : p.h) * a.kh + j * a.kn + 2 * lane, v);
+        });
 }
 
 ItemMap item_map(const WinArgs& a, int heads) {

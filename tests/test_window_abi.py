@@ -138,3 +138,12 @@ def test_binding_refuses_cpu_tensors(L):
                  lambda: psk.window_decode_step(x[:, :, 0], x[:, :, 0], x[:, :, 0], x, x, torch.zeros(1, dtype=torch.int32), 8)):
         with pytest.raises(RuntimeError, match="CUDA"):
             call()
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("B,H,Hkv,n,window,sinks", [(100, 24, 8, 1, 7, 2), (1, 1, 1, 1, 1, 0), (3, 12, 12, 129, 60, 0), (2, 16, 2, 5000, 300, 16), (1, 8, 1, 700, 300, 0)])
+def test_the_backwards_workspace_serves_the_forward(L, dtype, B, H, Hkv, n, window, sinks):
+    for path in (0, 1):
+        s = WindowShape(B, H, Hkv, n, 64, window, sinks, dtype, path, 0.125, 64 * n * H, 64 * n, 64, 64 * n * Hkv, 64 * n, 64)
+        fwd, bwd = (L.psk_window_workspace_bytes(byref(s), k) for k in (0, 1))
+        assert 256 <= fwd <= bwd
