@@ -19,7 +19,7 @@ struct WinArgs {
     float* lse;
     float *stat_l, *stat_d;           // [B,H,n] scratch: -lse log2(e) and -D, written by the query side, read by the key side
     const int32_t* lengths;           // [B] or null
-    int* status;                      // the call's status word; its first kernel clears it
+    int* status;                      // the call's status word; its first kernel clears it (CUDA-core kernels)
     int B, H, Hkv, G, n, window, sinks;
     float scale, c;                   // c = scale log2(e)
     int64_t qb, qh, qn, kb, kh, kn;   // element strides of the query-side and of the key-side tensors

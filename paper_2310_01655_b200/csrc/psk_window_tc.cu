@@ -26,7 +26,7 @@ constexpr int kRows = 128;
 // Items
 // ---------------------------------------------------------------------------
 struct Item { int b, h, row0, len; };
-struct ItemMap { FastDiv tiles, heads, parts; };
+struct ItemMap { FastDiv tiles, heads, parts; bool takes; };      // takes: there are more items than places for CTAs
 __device__ __forceinline__ Item item_of(const WinArgs& a, const ItemMap& m, int index) {
     const int bh = m.tiles.div(index);
     Item p;
@@ -37,7 +37,7 @@ __device__ __forceinline__ Item item_of(const WinArgs& a, const ItemMap& m, int 
     return p;
 }
 
-// The items of a CTA: its own index first, then those that it takes over.  The answer behind the it-th item is asked for by the
+// The items of a CTA: its own index first, then, where there are more items than places, those that it takes over.  The answer behind the it-th item is asked for by the
 // loading warp while that item is worked on, and read by every warp.
 struct Sched {
     ulonglong2 answer[2];
@@ -48,14 +48,15 @@ __device__ __forceinline__ void sched_init(Sched& s, int warps) {
 }
 // may the place of the it-th answer be written again?
 __device__ __forceinline__ bool sched_free(Sched& s, int it, int* status) { return it < 2 || mbar_wait(&s.taken[it & 1], (it / 2 - 1) & 1, status, kErrMma); }
-__device__ __forceinline__ void sched_ask(Sched& s, int it) {
+__device__ __forceinline__ void sched_ask(Sched& s, int it, bool takes) {
+    if (!takes) return;
     mbar_expect_tx(&s.full[it & 1], 16);
     asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];"
                  ::"r"(smem_u32(&s.answer[it & 1])), "r"(smem_u32(&s.full[it & 1])) : "memory");
 }
 // The index of the item behind the it-th; -1: there is none, or a wait gave up.  Followed by sched_taken() from one lane of the warp.
-__device__ __forceinline__ int sched_next(Sched& s, int it, int* status) {
-    if (!mbar_wait(&s.full[it & 1], (it / 2) & 1, status, kErrTma)) return -1;
+__device__ __forceinline__ int sched_next(Sched& s, int it, bool takes, int* status) {
+    if (!takes || !mbar_wait(&s.full[it & 1], (it / 2) & 1, status, kErrTma)) return -1;
     uint64_t lo, hi;
     asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(lo), "=l"(hi) : "r"(smem_u32(&s.answer[it & 1])) : "memory");
     uint32_t got, index;
@@ -242,7 +243,7 @@ tc_win_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
     }
     if (tid < 8) s_redo[tid] = kNoItem;
     pdl_sync();
-    if (blockIdx.x == 0 && tid == 0) *status = 0;
+    if (!map.takes && blockIdx.x == 0 && tid == 0) *status = 0;
     if (warp == Fwd::kMma) { tmem_alloc(&tm_slot, Fwd::kTmem); tmem_relinquish(); }
     tc_fence_before();
     __syncthreads();
@@ -256,7 +257,7 @@ tc_win_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
         for (int it = 0, index = blockIdx.x; index >= 0 && ok; ++it) {
             ok = __all_sync(0xffffffffu, sched_free(sched, it, status));
             if (!ok) break;
-            if (elect_one()) sched_ask(sched, it);
+            if (elect_one()) sched_ask(sched, it, map.takes);
             const Item p = item_of(a, map, index);
             if (p.row0 < p.len) {
                 const int buf = items & 1;
@@ -296,7 +297,7 @@ tc_win_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
                 }
                 if (!ok) break;
             }
-            index = sched_next(sched, it, status);
+            index = sched_next(sched, it, map.takes, status);
             __syncwarp();
             if (tid % 32 == 0) sched_taken(sched, it);
         }
@@ -342,7 +343,7 @@ tc_win_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
                     product(t - 1);                       // (nobody waits for an item that asks for nothing)
                 }
                 if (!ok) break;
-                index = sched_next(sched, it, status);
+                index = sched_next(sched, it, map.takes, status);
                 sched_taken(sched, it);
             }
             if (ok && owed) product(t - 1);
@@ -460,7 +461,7 @@ tc_win_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
                 zero_tile<Fwd::kRowThreads>((bf16*)a.out + p.b * a.qb + p.h * a.qh, a.qn, p.row0, a.n, tid);
                 if (half == 0 && i < a.n) lse[i] = neg_inf();
             }
-            index = sched_next(sched, it, status);
+            index = sched_next(sched, it, map.takes, status);
             if (bar_any(5, Fwd::kRowThreads, index < 0)) index = -1;        // (all of them or none: they share barriers)
             if (lane == 0) sched_taken(sched, it);
         }
@@ -538,7 +539,7 @@ tc_win_dq_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
     }
     if (tid < 4 * kGroups) s_redo[tid] = kNoItem;
     pdl_sync();
-    if (blockIdx.x == 0 && tid == 0) *status = 0;
+    if (!map.takes && blockIdx.x == 0 && tid == 0) *status = 0;
     if (warp == Dq::kMma) { tmem_alloc(&tm_slot, Dq::kTmem); tmem_relinquish(); }
     tc_fence_before();
     __syncthreads();
@@ -573,10 +574,10 @@ tc_win_dq_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
         for (int it = 0; index >= 0 && ok; ++it) {
             ok = __all_sync(0xffffffffu, sched_free(sched, it, status));
             if (!ok) break;
-            if (elect_one()) sched_ask(sched, it);
+            if (elect_one()) sched_ask(sched, it, map.takes);
             Item ahead = p;
             auto look_ahead = [&]() {
-                index = sched_next(sched, it, status);
+                index = sched_next(sched, it, map.takes, status);
                 __syncwarp();
                 if (lane == 0) sched_taken(sched, it);
                 if (index < 0) return;
@@ -661,7 +662,7 @@ tc_win_dq_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
                 }
                 while (ok && w.done < begun) product();
                 if (!ok) break;
-                index = sched_next(sched, it, status);
+                index = sched_next(sched, it, map.takes, status);
                 sched_taken(sched, it);
             }
             while (ok && w.done < w.t) product();
@@ -751,7 +752,7 @@ tc_win_dq_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
             } else if (group == 0) {
                 zero_tile<kRows>((bf16*)a.dQ + qoff, a.qn, p.row0, a.n, row);
             }
-            index = sched_next(sched, it, status);
+            index = sched_next(sched, it, map.takes, status);
             if (bar_any(1 + group, kRows, index < 0)) index = -1;            // (a whole warpgroup or none of it: it shares barriers)
             if (lane == 0) sched_taken(sched, it);
         }
@@ -834,7 +835,7 @@ tc_win_dkv_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constan
         for (int it = 0, index = blockIdx.x; index >= 0 && ok; ++it) {
             ok = __all_sync(0xffffffffu, sched_free(sched, it, status));
             if (!ok) break;
-            if (elect_one()) sched_ask(sched, it);
+            if (elect_one()) sched_ask(sched, it, map.takes);
             const KeyItem p = item(index);
             if (!p.empty()) {
                 const int kv = items & 1, tiles = tiles_of(p), steps = tiles * a.G;
@@ -883,7 +884,7 @@ tc_win_dkv_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constan
                 }
                 if (!ok) break;
             }
-            index = sched_next(sched, it, status);
+            index = sched_next(sched, it, map.takes, status);
             __syncwarp();
             if (lane == 0) sched_taken(sched, it);
         }
@@ -934,7 +935,7 @@ tc_win_dkv_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constan
                 }
                 while (ok && w.done < begun) product();
                 if (!ok) break;
-                index = sched_next(sched, it, status);
+                index = sched_next(sched, it, map.takes, status);
                 sched_taken(sched, it);
             }
             while (ok && w.done < w.t) product();
@@ -1028,7 +1029,7 @@ tc_win_dkv_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constan
             } else if (group < 2 && p.part <= 0 && (!PARTS || a.hs == 1)) {
                 zero_tile<kRows>((bf16*)(group == 0 ? a.dK : a.dV) + p.b * a.kb + p.h * a.kh, a.kn, p.key0, a.n, row);
             }
-            index = sched_next(sched, it, status);
+            index = sched_next(sched, it, map.takes, status);
             if (bar_any(1 + group, kRows, index < 0)) index = -1;            // (a whole warpgroup or none of it: it shares barriers)
             if (lane == 0) sched_taken(sched, it);
         }
@@ -1050,8 +1051,20 @@ tc_win_dkv_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constan
         });
 }
 
-ItemMap item_map(const WinArgs& a, int heads) {
+// The status word, in front of a kernel whose CTAs take over items: any item that has not been started may be taken over, the first one too, so
+// that none of its CTAs is sure to clear the word, nor to do so before another may write it.
+__global__ void win_clear_kernel(int* status) {
+    pdl_sync();
+    *status = 0;
+}
+void clear_status(int* status, cudaStream_t s) {
+    prof_begin("win_clear_kernel", s);
+    launch_pdl(win_clear_kernel, dim3(1), dim3(1), 0, s, status);
+    prof_end(s);
+}
+ItemMap item_map(const WinArgs& a, int heads, unsigned items, int per_sm) {
     ItemMap m;
+    m.takes = items > 148u * per_sm;
     m.tiles.set((uint32_t)((a.n + kRows - 1) / kRows));
     m.heads.set((uint32_t)heads);
     m.parts.set((uint32_t)(a.parts > 0 ? a.parts : 1));
@@ -1066,9 +1079,11 @@ cudaError_t tc_window_fwd(const WinArgs& a, int* status, cudaStream_t s) {
     CUtensorMap mQ, mK, mV, mO;
     if (!map_q(a, &mQ, a.Q, 128) || !map_k(a, &mK, a.K, 128) || !map_k(a, &mV, a.V, 128) || !map_q(a, &mO, a.out, 128)) return cudaErrorInvalidValue;
     PSK_TRY(set_smem(tc_win_fwd_kernel, Fwd::bytes));
-    const unsigned tiles = (unsigned)((a.n + kRows - 1) / kRows);
+    const unsigned items = (unsigned)((a.n + kRows - 1) / kRows) * a.B * a.H;
+    const ItemMap map = item_map(a, a.H, items, Fwd::kPerSm);
+    if (map.takes) clear_status(status, s);
     prof_begin("tc_win_fwd_kernel", s);
-    launch_pdl(tc_win_fwd_kernel, dim3(tiles * a.B * a.H), dim3(Fwd::kThreads), Fwd::bytes, s, mQ, mK, mV, mO, a, item_map(a, a.H), status);
+    launch_pdl(tc_win_fwd_kernel, dim3(items), dim3(Fwd::kThreads), Fwd::bytes, s, mQ, mK, mV, mO, a, map, status);
     prof_end(s);
     return cudaGetLastError();
 }
@@ -1080,8 +1095,11 @@ cudaError_t tc_window_bwd(const WinArgs& a, const WinArgs& k, int* status, cudaS
         if (!map_q(a, &mQ, a.Q, 128) || !map_q(a, &mG, a.dO, 128) || !map_q(a, &mO, a.O, 128) || !map_k(a, &mK, a.K, 64) || !map_k(a, &mV, a.V, 64) || !map_q(a, &mDq, a.dQ, 128))
             return cudaErrorInvalidValue;
         PSK_TRY(set_smem(tc_win_dq_kernel, Dq::bytes));
+        const unsigned items = tiles * a.B * a.H;
+        const ItemMap map = item_map(a, a.H, items, 1);
+        if (map.takes) clear_status(status, s);
         prof_begin("tc_win_dq_kernel", s);
-        launch_pdl(tc_win_dq_kernel, dim3(tiles * a.B * a.H), dim3(Dq::kThreads), Dq::bytes, s, mQ, mG, mO, mK, mV, mDq, a, item_map(a, a.H), status);
+        launch_pdl(tc_win_dq_kernel, dim3(items), dim3(Dq::kThreads), Dq::bytes, s, mQ, mG, mO, mK, mV, mDq, a, map, status);
         prof_end(s);
     }
     CUtensorMap mK, mV, mQ, mG, mDk, mDv;
@@ -1090,8 +1108,9 @@ cudaError_t tc_window_bwd(const WinArgs& a, const WinArgs& k, int* status, cudaS
         return cudaErrorInvalidValue;
     const auto dkv = k.parts > 0 || k.hs > 1 ? tc_win_dkv_kernel<true> : tc_win_dkv_kernel<false>;
     PSK_TRY(set_smem(dkv, Dkv::bytes));
+    const unsigned items = (tiles + k.parts) * k.B * k.Hkv;
     prof_begin("tc_win_dkv_kernel", s);
-    launch_pdl(dkv, dim3((tiles + k.parts) * k.B * k.Hkv), dim3(Dkv::kThreads), Dkv::bytes, s, mK, mV, mQ, mG, mDk, mDv, k, item_map(k, k.Hkv), status);
+    launch_pdl(dkv, dim3(items), dim3(Dkv::kThreads), Dkv::bytes, s, mK, mV, mQ, mG, mDk, mDv, k, item_map(k, k.Hkv, items, 1), status);
     prof_end(s);
     return cudaGetLastError();
 }
