@@ -26,7 +26,7 @@ constexpr int kRows = 128;
 // Items
 // ---------------------------------------------------------------------------
 struct Item { int b, h, row0, len; };
-struct ItemMap { FastDiv tiles, heads, parts; bool takes; };      // takes: there are more items than places for CTAs
+struct ItemMap { FastDiv tiles, heads, parts; };
 __device__ __forceinline__ Item item_of(const WinArgs& a, const ItemMap& m, int index) {
     const int bh = m.tiles.div(index);
     Item p;
@@ -37,7 +37,7 @@ __device__ __forceinline__ Item item_of(const WinArgs& a, const ItemMap& m, int 
     return p;
 }
 
-// The items of a CTA: its own index first, then, where there are more items than places, those that it takes over.  The answer behind the it-th item is asked for by the
+// The items of a CTA: its own index first, then, where there are more items than places (`takes`), those that it takes over.  The answer behind the it-th item is asked for by the
 // loading warp while that item is worked on, and read by every warp.
 struct Sched {
     ulonglong2 answer[2];
@@ -220,6 +220,7 @@ struct Fwd {
     static constexpr uint32_t kTmem = 256, cS = 0, cP = 128, cO = 192;
 };
 
+template <bool TAKES>
 __global__ void __launch_bounds__(Fwd::kThreads, Fwd::kPerSm)
 tc_win_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV,
                   const __grid_constant__ CUtensorMap mapO, const __grid_constant__ WinArgs a, const __grid_constant__ ItemMap map, int* status) {
@@ -243,7 +244,7 @@ tc_win_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
     }
     if (tid < 8) s_redo[tid] = kNoItem;
     pdl_sync();
-    if (!map.takes && blockIdx.x == 0 && tid == 0) *status = 0;
+    if (!TAKES && blockIdx.x == 0 && tid == 0) *status = 0;
     if (warp == Fwd::kMma) { tmem_alloc(&tm_slot, Fwd::kTmem); tmem_relinquish(); }
     tc_fence_before();
     __syncthreads();
@@ -257,7 +258,7 @@ tc_win_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
         for (int it = 0, index = blockIdx.x; index >= 0 && ok; ++it) {
             ok = __all_sync(0xffffffffu, sched_free(sched, it, status));
             if (!ok) break;
-            if (elect_one()) sched_ask(sched, it, map.takes);
+            if (elect_one()) sched_ask(sched, it, TAKES);
             const Item p = item_of(a, map, index);
             if (p.row0 < p.len) {
                 const int buf = items & 1;
@@ -297,7 +298,7 @@ tc_win_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
                 }
                 if (!ok) break;
             }
-            index = sched_next(sched, it, map.takes, status);
+            index = sched_next(sched, it, TAKES, status);
             __syncwarp();
             if (tid % 32 == 0) sched_taken(sched, it);
         }
@@ -343,7 +344,7 @@ tc_win_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
                     product(t - 1);                       // (nobody waits for an item that asks for nothing)
                 }
                 if (!ok) break;
-                index = sched_next(sched, it, map.takes, status);
+                index = sched_next(sched, it, TAKES, status);
                 sched_taken(sched, it);
             }
             if (ok && owed) product(t - 1);
@@ -461,7 +462,7 @@ tc_win_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
                 zero_tile<Fwd::kRowThreads>((bf16*)a.out + p.b * a.qb + p.h * a.qh, a.qn, p.row0, a.n, tid);
                 if (half == 0 && i < a.n) lse[i] = neg_inf();
             }
-            index = sched_next(sched, it, map.takes, status);
+            index = sched_next(sched, it, TAKES, status);
             if (bar_any(5, Fwd::kRowThreads, index < 0)) index = -1;        // (all of them or none: they share barriers)
             if (lane == 0) sched_taken(sched, it);
         }
@@ -515,6 +516,7 @@ struct Dq {
     static constexpr uint32_t kTmem = 512, cDq = 0, cS = 64;                   // cS + 128 warpgroup: S (ds), dP
 };
 
+template <bool TAKES>
 __global__ void __launch_bounds__(Dq::kThreads, 1)
 tc_win_dq_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapG, const __grid_constant__ CUtensorMap mapO,
                  const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV, const __grid_constant__ CUtensorMap mapDq, const __grid_constant__ WinArgs a,
@@ -539,7 +541,7 @@ tc_win_dq_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
     }
     if (tid < 4 * kGroups) s_redo[tid] = kNoItem;
     pdl_sync();
-    if (!map.takes && blockIdx.x == 0 && tid == 0) *status = 0;
+    if (!TAKES && blockIdx.x == 0 && tid == 0) *status = 0;
     if (warp == Dq::kMma) { tmem_alloc(&tm_slot, Dq::kTmem); tmem_relinquish(); }
     tc_fence_before();
     __syncthreads();
@@ -574,10 +576,10 @@ tc_win_dq_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
         for (int it = 0; index >= 0 && ok; ++it) {
             ok = __all_sync(0xffffffffu, sched_free(sched, it, status));
             if (!ok) break;
-            if (elect_one()) sched_ask(sched, it, map.takes);
+            if (elect_one()) sched_ask(sched, it, TAKES);
             Item ahead = p;
             auto look_ahead = [&]() {
-                index = sched_next(sched, it, map.takes, status);
+                index = sched_next(sched, it, TAKES, status);
                 __syncwarp();
                 if (lane == 0) sched_taken(sched, it);
                 if (index < 0) return;
@@ -662,7 +664,7 @@ tc_win_dq_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
                 }
                 while (ok && w.done < begun) product();
                 if (!ok) break;
-                index = sched_next(sched, it, map.takes, status);
+                index = sched_next(sched, it, TAKES, status);
                 sched_taken(sched, it);
             }
             while (ok && w.done < w.t) product();
@@ -752,7 +754,7 @@ tc_win_dq_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
             } else if (group == 0) {
                 zero_tile<kRows>((bf16*)a.dQ + qoff, a.qn, p.row0, a.n, row);
             }
-            index = sched_next(sched, it, map.takes, status);
+            index = sched_next(sched, it, TAKES, status);
             if (bar_any(1 + group, kRows, index < 0)) index = -1;            // (a whole warpgroup or none of it: it shares barriers)
             if (lane == 0) sched_taken(sched, it);
         }
@@ -835,7 +837,7 @@ tc_win_dkv_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constan
         for (int it = 0, index = blockIdx.x; index >= 0 && ok; ++it) {
             ok = __all_sync(0xffffffffu, sched_free(sched, it, status));
             if (!ok) break;
-            if (elect_one()) sched_ask(sched, it, map.takes);
+            if (elect_one()) sched_ask(sched, it, true);
             const KeyItem p = item(index);
             if (!p.empty()) {
                 const int kv = items & 1, tiles = tiles_of(p), steps = tiles * a.G;
@@ -884,7 +886,7 @@ tc_win_dkv_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constan
                 }
                 if (!ok) break;
             }
-            index = sched_next(sched, it, map.takes, status);
+            index = sched_next(sched, it, true, status);
             __syncwarp();
             if (lane == 0) sched_taken(sched, it);
         }
@@ -935,7 +937,7 @@ tc_win_dkv_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constan
                 }
                 while (ok && w.done < begun) product();
                 if (!ok) break;
-                index = sched_next(sched, it, map.takes, status);
+                index = sched_next(sched, it, true, status);
                 sched_taken(sched, it);
             }
             while (ok && w.done < w.t) product();
@@ -1029,7 +1031,7 @@ tc_win_dkv_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constan
             } else if (group < 2 && p.part <= 0 && (!PARTS || a.hs == 1)) {
                 zero_tile<kRows>((bf16*)(group == 0 ? a.dK : a.dV) + p.b * a.kb + p.h * a.kh, a.kn, p.key0, a.n, row);
             }
-            index = sched_next(sched, it, map.takes, status);
+            index = sched_next(sched, it, true, status);
             if (bar_any(1 + group, kRows, index < 0)) index = -1;            // (a whole warpgroup or none of it: it shares barriers)
             if (lane == 0) sched_taken(sched, it);
         }
@@ -1062,9 +1064,8 @@ void clear_status(int* status, cudaStream_t s) {
     launch_pdl(win_clear_kernel, dim3(1), dim3(1), 0, s, status);
     prof_end(s);
 }
-ItemMap item_map(const WinArgs& a, int heads, unsigned items, int per_sm) {
+ItemMap item_map(const WinArgs& a, int heads) {
     ItemMap m;
-    m.takes = items > 148u * per_sm;
     m.tiles.set((uint32_t)((a.n + kRows - 1) / kRows));
     m.heads.set((uint32_t)heads);
     m.parts.set((uint32_t)(a.parts > 0 ? a.parts : 1));
@@ -1078,12 +1079,13 @@ bool map_k(const WinArgs& a, CUtensorMap* m, const void* p, int rows) { return t
 cudaError_t tc_window_fwd(const WinArgs& a, int* status, cudaStream_t s) {
     CUtensorMap mQ, mK, mV, mO;
     if (!map_q(a, &mQ, a.Q, 128) || !map_k(a, &mK, a.K, 128) || !map_k(a, &mV, a.V, 128) || !map_q(a, &mO, a.out, 128)) return cudaErrorInvalidValue;
-    PSK_TRY(set_smem(tc_win_fwd_kernel, Fwd::bytes));
     const unsigned items = (unsigned)((a.n + kRows - 1) / kRows) * a.B * a.H;
-    const ItemMap map = item_map(a, a.H, items, Fwd::kPerSm);
-    if (map.takes) clear_status(status, s);
+    const bool takes = items > 148u * Fwd::kPerSm;
+    const auto fwd = takes ? tc_win_fwd_kernel<true> : tc_win_fwd_kernel<false>;
+    PSK_TRY(set_smem(fwd, Fwd::bytes));
+    if (takes) clear_status(status, s);
     prof_begin("tc_win_fwd_kernel", s);
-    launch_pdl(tc_win_fwd_kernel, dim3(items), dim3(Fwd::kThreads), Fwd::bytes, s, mQ, mK, mV, mO, a, map, status);
+    launch_pdl(fwd, dim3(items), dim3(Fwd::kThreads), Fwd::bytes, s, mQ, mK, mV, mO, a, item_map(a, a.H), status);
     prof_end(s);
     return cudaGetLastError();
 }
@@ -1094,12 +1096,13 @@ cudaError_t tc_window_bwd(const WinArgs& a, const WinArgs& k, int* status, cudaS
         CUtensorMap mQ, mG, mO, mK, mV, mDq;
         if (!map_q(a, &mQ, a.Q, 128) || !map_q(a, &mG, a.dO, 128) || !map_q(a, &mO, a.O, 128) || !map_k(a, &mK, a.K, 64) || !map_k(a, &mV, a.V, 64) || !map_q(a, &mDq, a.dQ, 128))
             return cudaErrorInvalidValue;
-        PSK_TRY(set_smem(tc_win_dq_kernel, Dq::bytes));
         const unsigned items = tiles * a.B * a.H;
-        const ItemMap map = item_map(a, a.H, items, 1);
-        if (map.takes) clear_status(status, s);
+        const bool takes = items > 148u;
+        const auto dq = takes ? tc_win_dq_kernel<true> : tc_win_dq_kernel<false>;
+        PSK_TRY(set_smem(dq, Dq::bytes));
+        if (takes) clear_status(status, s);
         prof_begin("tc_win_dq_kernel", s);
-        launch_pdl(tc_win_dq_kernel, dim3(items), dim3(Dq::kThreads), Dq::bytes, s, mQ, mG, mO, mK, mV, mDq, a, map, status);
+        launch_pdl(dq, dim3(items), dim3(Dq::kThreads), Dq::bytes, s, mQ, mG, mO, mK, mV, mDq, a, item_map(a, a.H), status);
         prof_end(s);
     }
     CUtensorMap mK, mV, mQ, mG, mDk, mDv;
@@ -1108,9 +1111,8 @@ cudaError_t tc_window_bwd(const WinArgs& a, const WinArgs& k, int* status, cudaS
         return cudaErrorInvalidValue;
     const auto dkv = k.parts > 0 || k.hs > 1 ? tc_win_dkv_kernel<true> : tc_win_dkv_kernel<false>;
     PSK_TRY(set_smem(dkv, Dkv::bytes));
-    const unsigned items = (tiles + k.parts) * k.B * k.Hkv;
     prof_begin("tc_win_dkv_kernel", s);
-    launch_pdl(dkv, dim3(items), dim3(Dkv::kThreads), Dkv::bytes, s, mK, mV, mQ, mG, mDk, mDv, k, item_map(k, k.Hkv, items, 1), status);
+    launch_pdl(dkv, dim3((tiles + k.parts) * k.B * k.Hkv), dim3(Dkv::kThreads), Dkv::bytes, s, mK, mV, mQ, mG, mDk, mDv, k, item_map(k, k.Hkv), status);
     prof_end(s);
     return cudaGetLastError();
 }

@@ -22,11 +22,11 @@ def test_the_status_word_is_cleared_where_no_cta_may_be_taken_over():
     text = source(NAME)
     for name, body in kernels().items():
         clears = re.findall(r"[^\n]*\*status = 0;", body)
-        assert all("!map.takes" in c for c in clears), name
+        assert all("!TAKES" in c for c in clears), name
         assert bool(clears) == (name != "tc_win_dkv_kernel"), name                 # (the key side follows the query side)
-    for kernel in ("tc_win_fwd_kernel", "tc_win_dq_kernel"):
-        launch = text.index("launch_pdl(" + kernel)
-        assert "if (map.takes) clear_status(status, s);" in text[launch - 400:launch], kernel
+    for kernel, short in (("tc_win_fwd_kernel", "fwd"), ("tc_win_dq_kernel", "dq")):
+        launch = text.index("launch_pdl(%s," % short)
+        assert "takes ? %s<true> : %s<false>;" % (kernel, kernel) in text[launch - 400:launch] and "if (takes) clear_status(status, s);" in text[launch - 400:launch], kernel
     # and without items to take over nobody asks
     assert re.search(r"void sched_ask\([^)]*bool takes\) \{\s*if \(!takes\) return;", text)
     assert re.search(r"int sched_next\([^)]*bool takes[^)]*\) \{\s*if \(!takes \|\| ", text)
