@@ -683,6 +683,12 @@ def _window_scale(scale, h):
     return h ** -0.5 if scale is None else scale
 
 
+def _window_numbers(where, *values):
+    # (a descriptor's fields would take such a value modulo 2^32)
+    if not all(-2**31 <= v < 2**31 for v in values):
+        raise PskError(-3, where)
+
+
 def make_window_shape(Q, K, window, sinks=0, scale=None, path=PATH_AUTO) -> WindowShape:
     """Shape descriptor for [B,H,n,h] queries and [B,Hkv,n,h] keys (whose strides stand for all tensors of their side)."""
     for x in (Q, K):
@@ -692,6 +698,7 @@ def make_window_shape(Q, K, window, sinks=0, scale=None, path=PATH_AUTO) -> Wind
     if K.dtype != Q.dtype or (K.shape[0], K.shape[2], K.shape[3]) != (Q.shape[0], Q.shape[2], Q.shape[3]):
         raise ValueError("window attention: queries and keys must agree in dtype, batch, length and head dimension")
     B, H, n, h = Q.shape
+    _window_numbers("window attention", B, H, K.shape[1], n, h, window, sinks, path)
     return WindowShape(B, H, K.shape[1], n, h, window, sinks, _DTYPES[Q.dtype], path, _window_scale(scale, h), *Q.stride()[:3], *K.stride()[:3])
 
 
@@ -804,6 +811,7 @@ def window_decode_step(q, k, v, Kc, Vc, positions, window, sinks=0, scale=None, 
     _per_sequence("positions", q, positions)
     _check_cache(where, q, k.shape[1], Kc, Vc, window, sinks)
     B, H, h = q.shape
+    _window_numbers(where, B, H, k.shape[1], h, window, sinks)
     shp = WindowShape(B, H, k.shape[1], 1, h, window, sinks, _DTYPES[q.dtype], PATH_AUTO, _window_scale(scale, h), 0, 0, 0, 0, 0, 0)
     with torch.cuda.device(q.device):
         o = torch.empty_like(q) if out is None else out

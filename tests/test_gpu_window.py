@@ -431,3 +431,19 @@ def test_refusals():
         assert e.value.code == code
     with pytest.raises(RuntimeError):
         psk.window_attn_fwd(Q, K.cpu(), V.cpu(), 8)
+
+
+def test_windows_beyond_32_bits():
+    Q, K, V, dO = make("bf16", 1, 2, 1, 40)
+    O, lse = psk.window_attn_fwd(Q, K, V, 2**31 - 1, 2**31 - 1)
+    q, k, v = Q[:, :, 0], K[:, :, 0], V[:, :, 0]
+    Kc, Vc = psk.window_cache(1, 1, 8)
+    pos = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for window, sinks in ((2**32 + 8, 0), (8, 2**32), (2**31, 0)):
+        for call in (lambda: psk.window_attn_fwd(Q, K, V, window, sinks), lambda: psk.window_attn_bwd(Q, K, V, O, lse, dO, window, sinks)):
+            with pytest.raises(psk.PskError) as e:
+                call()
+            assert e.value.code == -3
+        for call in (lambda: psk.window_decode_step(q, k, v, Kc, Vc, pos, window, sinks), lambda: psk.window_cache_fill(K, V, Kc, Vc, window, sinks)):
+            with pytest.raises((psk.PskError, ValueError)):
+                call()

@@ -147,3 +147,22 @@ def test_the_backwards_workspace_serves_the_forward(L, dtype, B, H, Hkv, n, wind
         s = WindowShape(B, H, Hkv, n, 64, window, sinks, dtype, path, 0.125, 64 * n * H, 64 * n, 64, 64 * n * Hkv, 64 * n, 64)
         fwd, bwd = (L.psk_window_workspace_bytes(byref(s), k) for k in (0, 1))
         assert 256 <= fwd <= bwd
+
+
+@pytest.mark.parametrize("numbers", [dict(window=2**32 + 5), dict(window=2**31), dict(window=5, sinks=2**32), dict(window=5, sinks=2**40 + 1), dict(window=-2**32 + 5),
+                                     dict(window=5, path=2**32 + 1)])
+def test_numbers_beyond_32_bits(numbers):
+    """A descriptor's fields would take them modulo 2^32: another window, and no error."""
+    x = torch.zeros(1, 2, 8, 64)
+    with pytest.raises(psk.PskError) as e:
+        psk.binding.make_window_shape(x, x, **numbers)
+    assert e.value.code == -3
+
+
+def test_extents_beyond_32_bits():
+    for x in (torch.zeros(1, 1, 1, 64).expand(2**32 + 1, 1, 1, 64), torch.zeros(1, 1, 1, 64).expand(1, 1, 2**31, 64)):
+        with pytest.raises(psk.PskError) as e:
+            psk.binding.make_window_shape(x, x, 5)
+        assert e.value.code == -3
+    s = psk.binding.make_window_shape(torch.zeros(1, 2, 8, 64), torch.zeros(1, 1, 8, 64), 2**31 - 1, 2**31 - 1)
+    assert (s.window, s.sinks) == (2**31 - 1, 2**31 - 1)
