@@ -598,6 +598,16 @@ def _norm_rows(where, x):
     return [1] * fill + list(x.shape[:-1]), [0] * fill + list(x.stride()[:-1])
 
 
+def _rows_like(x):
+    """Uninitialised rows for a result of x's shape: in x's strides too, or contiguous where x's own rows overlap (expanded, for one)."""
+    end = x.shape[-1] if x.dim() else 1
+    for size, stride in sorted(((n, s) for n, s in zip(x.shape[:-1], x.stride()[:-1]) if n > 1), key=lambda e: e[1]):
+        if stride < end:
+            return torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        end += stride * (size - 1)
+    return _empty_like(x)
+
+
 def _norm_shape(where, x, eps, *others):
     for t in others:
         if t.shape != x.shape or t.dtype != x.dtype:
@@ -629,7 +639,8 @@ def _bytes_workspace(where, need, workspace, x):
 
 def layer_norm_fwd(X, gain=None, bias=None, eps=1e-6, out=None):
     """psk_layer_norm_fwd: (X - mean) / sqrt(var + eps) * gain + bias over the last dimension; X [.., cols] with at most
-    three leading dimensions of any strides, gain and bias fp32 [cols] or None.  `out` may be X."""
+    three leading dimensions of any strides, gain and bias fp32 [cols] or None.  `out` may be X; without it the result has X's strides, or is
+    contiguous where X's rows overlap."""
     res = (_fast or _native()).layer_norm_fwd(X, gain, bias, eps, out)
     if res is not None:
         return _result(res, "psk_layer_norm_fwd")
@@ -638,7 +649,7 @@ def layer_norm_fwd(X, gain=None, bias=None, eps=1e-6, out=None):
     _storage(where, X)
     _norm_params(where, X, gain, bias)
     with torch.cuda.device(X.device):
-        Y = _empty_like(X) if out is None else out
+        Y = _rows_like(X) if out is None else out
         shp = _norm_shape(where, X, eps, Y)
         st = lib().psk_layer_norm_fwd(byref(shp), _ptr(X), _ptr(gain), _ptr(bias), _ptr(Y), _stream())
     if st != 0:
@@ -657,7 +668,7 @@ def layer_norm_workspace_bytes(X) -> int:
 
 def layer_norm_bwd(X, gain, dY, eps=1e-6, params=True, workspace=None, out=None):
     """psk_layer_norm_bwd: returns (dX, dgain, dbias) from the forward's X and gain; dgain and dbias (fp32) are None
-    with params = False.  `out` (dX) may be X or dY."""
+    with params = False.  `out` (dX) may be X or dY; without it as in layer_norm_fwd."""
     res = (_fast or _native()).layer_norm_bwd(X, gain, dY, eps, params, workspace, out)
     if res is not None:
         return _result(res, "psk_layer_norm_bwd")
@@ -666,7 +677,7 @@ def layer_norm_bwd(X, gain, dY, eps=1e-6, params=True, workspace=None, out=None)
     _storage(where, X)
     _norm_params(where, X, gain)
     with torch.cuda.device(X.device):
-        dX = _empty_like(X) if out is None else out
+        dX = _rows_like(X) if out is None else out
         shp = _norm_shape(where, X, eps, dY, dX)
         dgain = dbias = None
         ws, nbytes = None, 0

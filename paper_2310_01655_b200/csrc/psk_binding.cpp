@@ -284,6 +284,21 @@ bool rows_of(const Tensor& x, int32_t (&n)[3], int64_t (&s)[3]) {
     }
     return x.size(d) <= INT32_MAX;
 }
+// Rows for a result of x's shape: in x's strides too, or contiguous where x's own rows overlap (expanded, for one).
+Tensor rows_like(const Tensor& x) {
+    const int64_t d = x.dim() - 1;
+    int64_t end = x.size(d);
+    bool used[3] = {false, false, false};                 // (rows_of: at most three leading dimensions)
+    for (;;) {
+        int at = -1;
+        for (int i = 0; i < d; ++i)
+            if (!used[i] && x.size(i) > 1 && (at < 0 || x.stride(i) < x.stride(at))) at = i;
+        if (at < 0) return empty_as(x);
+        if (x.stride(at) < end) return empty(x.sizes(), x.scalar_type(), x);
+        used[at] = true;
+        end += x.stride(at) * (x.size(at) - 1);
+    }
+}
 bool param_ok(const Tensor& x, const Tensor* p) {
     return p == nullptr || (on_device_of(x, p) && p->scalar_type() == at::kFloat && p->dim() == 1 && p->size(0) == x.size(-1) && p->is_contiguous());
 }
@@ -300,7 +315,7 @@ PyObject* layer_norm_fwd(PyObject* const* a, Py_ssize_t n) {
     int32_t e[3];
     if (!rows_of(*X, e, s.xs)) Py_RETURN_NONE;
     c10::cuda::CUDAGuard guard(X->device());
-    Tensor Y = out != nullptr ? *out : empty_as(*X);
+    Tensor Y = out != nullptr ? *out : rows_like(*X);
     if (!rows_of(Y, e, s.ys)) Py_RETURN_NONE;
     s.n0 = e[0]; s.n1 = e[1]; s.n2 = e[2]; s.cols = (int32_t)X->size(-1); s.dtype = dtype_of(*X); s.eps = (float)eps;
     int st;
@@ -325,7 +340,7 @@ PyObject* layer_norm_bwd(PyObject* const* a, Py_ssize_t n) {
     int32_t e[3];
     if (!rows_of(*X, e, s.xs) || !rows_of(*dY, e, s.ys)) Py_RETURN_NONE;
     c10::cuda::CUDAGuard guard(X->device());
-    Tensor dX = out != nullptr ? *out : empty_as(*X);
+    Tensor dX = out != nullptr ? *out : rows_like(*X);
     if (!rows_of(dX, e, s.zs)) Py_RETURN_NONE;
     s.n0 = e[0]; s.n1 = e[1]; s.n2 = e[2]; s.cols = (int32_t)X->size(-1); s.dtype = dtype_of(*X); s.eps = (float)eps;
     Tensor dg, db;

@@ -281,3 +281,21 @@ def test_an_output_of_other_strides(dtype, cols):
         dX, dgain, dbias = psk.layer_norm_bwd(X, gain, dY, out=dinto)
         assert dX is dinto or dX.data_ptr() == dinto.data_ptr()
         assert torch.equal(dinto, dXd) and torch.equal(dgain, dgd) and torch.equal(dbias, dbd)
+
+
+@pytest.mark.parametrize("native", [True, False])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_that_overlap(dtype, native, monkeypatch):
+    """Rows that are read may lie over one another; the results' do not."""
+    if not native:
+        monkeypatch.setattr(binding, "_fast", binding._NoNative())
+    base = rows_of(dtype, 3, 1, 5, 64, seed=41)
+    long = rows_of(dtype, 200, seed=42)
+    gain = 1 + 0.1 * rows_of("f32", 64, seed=3)
+    for X in (base.expand(3, 7, 5, 64), base[:1, :, :1].expand(2, 7, 5, 64), long.unfold(0, 64, 8), long.unfold(0, 64, 1)):
+        dY = rows_of(dtype, *X.shape, seed=43)
+        Y, (dX, dgain, dbias) = psk.layer_norm_fwd(X, gain), psk.layer_norm_bwd(X, gain, dY)
+        assert Y.is_contiguous() and dX.is_contiguous()
+        check(dtype, X, gain, None, dY, Y, dX, dgain, dbias)
+    X = rows_of(dtype, 4, 9, 5, 64, seed=44).permute(2, 0, 1, 3)[:, 1:, ::2]             # apart, in an order of their own
+    assert psk.layer_norm_fwd(X, gain).stride() == X.stride()
