@@ -363,8 +363,8 @@ int psk_check(const void* workspace, void* stream);
  * word.  `workspace`: DEVICE, at least 256 bytes, 256-byte aligned. */
 int psk_selftest_wait_timeout(void* workspace, size_t workspace_bytes, uint64_t limit_ns, void* stream);
 
-/* Number of kernel launches the last forward / backward call on this thread enqueued
- * (for launch accounting in benchmarks). */
+/* Number of kernel launches the last call on this thread enqueued: attention forward or backward, sketch, decode step,
+ * layer normalisation, window attention, its cache (for launch accounting in benchmarks). */
 int psk_last_launch_count(void);
 
 /* Measurement aid (no counterpart in the paper).  psk_profile_enable(1) makes every

@@ -13,8 +13,12 @@ namespace {
 struct ProfRec { const char* name; cudaEvent_t a, b; };
 bool g_prof_on = false;
 std::vector<ProfRec> g_prof;
+thread_local int g_last_launches = 0, g_begun = 0;        // of the last call; of all
 }  // namespace
+CountLaunches::CountLaunches() : before(g_begun) {}
+CountLaunches::~CountLaunches() { g_last_launches = g_begun - before; }
 void prof_begin(const char* name, cudaStream_t s) {
+    ++g_begun;
     if (!g_prof_on) return;
     ProfRec r{name, nullptr, nullptr};
     if (cudaEventCreate(&r.a) != cudaSuccess || cudaEventCreate(&r.b) != cudaSuccess) return;
@@ -28,8 +32,6 @@ void prof_end(cudaStream_t s) {
 }  // namespace psk
 
 namespace {
-
-thread_local int g_last_launches = 0;
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 

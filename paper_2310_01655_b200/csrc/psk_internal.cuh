@@ -117,6 +117,12 @@ cudaError_t tc_bwd(const Dims& d, const void* Q, const void* K, const void* V,
 // CUDA events on its own stream; disabled, these are no-ops.
 void prof_begin(const char* name, cudaStream_t s);
 void prof_end(cudaStream_t s);
+// The launches of a call, from here to its end, become what psk_last_launch_count() reports (each goes through prof_begin()).
+struct CountLaunches {
+    CountLaunches();
+    ~CountLaunches();
+    int before;
+};
 
 // Launches on a stream follow one another by programmatic dependence: a kernel may be put on the SMs as soon
 // as every CTA of the one before it has started, and waits in pdl_sync() until that one has ended and its

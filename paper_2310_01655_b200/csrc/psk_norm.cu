@@ -572,6 +572,7 @@ int psk_layer_norm_fwd(const psk_norm_shape* shape, const void* X, const float* 
     const int st = check_shape(shape, false);
     if (st != PSK_OK) return st;
     if (!X || !Y) return PSK_ERR_INVALID_ARG;
+    CountLaunches count;
     NormArgs a{};
     a.x = X; a.z = Y; a.gain = gain; a.bias = bias;
     return run(shape, a, false, (cudaStream_t)stream);
@@ -585,6 +586,7 @@ int psk_layer_norm_bwd(const psk_norm_shape* shape, const void* X, const float* 
     if (dgain != nullptr || dbias != nullptr) {
         if (!workspace || workspace_bytes < psk_layer_norm_workspace_bytes(shape) || (reinterpret_cast<uintptr_t>(workspace) & 15u)) return PSK_ERR_WORKSPACE;
     }
+    CountLaunches count;
     NormArgs a{};
     a.x = X; a.y = dY; a.z = dX; a.gain = gain; a.dgain = dgain; a.dbias = dbias;
     a.partial = static_cast<float*>(workspace);

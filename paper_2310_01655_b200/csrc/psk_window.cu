@@ -690,6 +690,7 @@ int psk_window_attn_fwd(const psk_window_shape* shape, const void* Q, const void
         if (!aligned16(p)) return PSK_ERR_ALIGN;
     if ((reinterpret_cast<uintptr_t>(lse) | reinterpret_cast<uintptr_t>(lengths)) & 3u) return PSK_ERR_ALIGN;
     if (!workspace || workspace_bytes < psk_window_workspace_bytes(shape, 0) || (reinterpret_cast<uintptr_t>(workspace) % kAlign)) return PSK_ERR_WORKSPACE;
+    CountLaunches count;
     cudaStream_t s = (cudaStream_t)stream;
     WinArgs a = args_of(shape);
     a.Q = Q; a.K = K; a.V = V; a.out = O; a.lse = lse; a.lengths = lengths;
@@ -714,6 +715,7 @@ int psk_window_attn_bwd(const psk_window_shape* shape, const void* Q, const void
         if (!aligned16(p)) return PSK_ERR_ALIGN;
     if ((reinterpret_cast<uintptr_t>(lse) | reinterpret_cast<uintptr_t>(lengths)) & 3u) return PSK_ERR_ALIGN;
     if (!workspace || workspace_bytes < psk_window_workspace_bytes(shape, 1) || (reinterpret_cast<uintptr_t>(workspace) % kAlign)) return PSK_ERR_WORKSPACE;
+    CountLaunches count;
     cudaStream_t s = (cudaStream_t)stream;
     WinArgs a = args_of(shape);
     a.Q = Q; a.K = K; a.V = V; a.O = O; a.lse_in = lse; a.dO = dO; a.dQ = dQ; a.dK = dK; a.dV = dV; a.lengths = lengths;

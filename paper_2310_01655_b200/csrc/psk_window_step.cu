@@ -529,6 +529,7 @@ int psk_window_cache_fill(const psk_window_shape* shape, const void* K, const vo
     const int per = shape->dtype == PSK_F32 ? 16 : 32;
     const int64_t grid = (a.total + per - 1) / per;
     if (grid >= (int64_t)1 << 31) return PSK_ERR_SHAPE;
+    CountLaunches count;
     cudaStream_t s = (cudaStream_t)stream;
     prof_begin("win_fill_kernel", s);
     if (shape->dtype == PSK_F32) launch_pdl(win_fill_kernel<float>, dim3((unsigned)grid), dim3(256), 0, s, a);
@@ -548,6 +549,7 @@ int psk_window_decode_step(const psk_window_shape* shape, const void* q, const v
     if (reinterpret_cast<uintptr_t>(positions) & 3u) return PSK_ERR_ALIGN;
     StepArgs a{q, k, v, Kc, Vc, o, positions, shape->H, shape->Hkv, shape->H / shape->Hkv, 1, shape->window, shape->sinks, shape->scale * kLog2e};
     const int64_t keyheads = (int64_t)shape->B * shape->Hkv;
+    CountLaunches count;
     cudaStream_t s = (cudaStream_t)stream;
     const cudaError_t e = shape->dtype == PSK_F32 ? launch_f32(a, keyheads, s) : launch_bf16(a, keyheads, s);
     return e == cudaSuccess ? PSK_OK : PSK_ERR_CUDA;

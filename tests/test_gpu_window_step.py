@@ -223,3 +223,31 @@ def test_refusals():
                  lambda: psk.window_cache_fill(x, x, Kc, Vc, 29, 2), lambda: psk.window_cache_fill(x, x, Kc, Vc, 30, 2, pos.long())):
         with pytest.raises(ValueError):
             call()
+
+
+def test_launches_are_counted():
+    """What the last call on this thread enqueued, not an earlier one."""
+    def launches(call):
+        call()
+        n = psk.last_launch_count()
+        assert n == psk.last_launch_count()
+        return n
+    Kc, Vc = psk.window_cache(2, 2, 30, 2)
+    Q, K, V = rand("bf16", 2, 4, 40, 64, seed=1), rand("bf16", 2, 2, 40, 64, seed=2), rand("bf16", 2, 2, 40, 64, seed=3)
+    G = rand("bf16", 1, 64, 16, seed=4)
+    X = rand("bf16", 1, 4, 128, 64, seed=5)
+    other = launches(lambda: psk.causal_attn_bwd(X, X, X, G, G, X, torch.ones(1, 4, 128, device="cuda"), X, 128))
+    assert other > 2
+    pos = torch.zeros(2, dtype=torch.int32, device="cuda")
+    O, lse = psk.window_attn_fwd(Q, K, V, 30, 2)
+    F = Q.float()
+    Kf = K.float()
+    Of, lf = psk.window_attn_fwd(F, Kf, Kf, 30)
+    for want, call in ((1, lambda: psk.window_attn_fwd(Q, K, V, 30, 2)), (2, lambda: psk.window_attn_bwd(F, F, F, F, torch.zeros(2, 4, 40, device="cuda"), F, 30)),
+                       (1, lambda: psk.window_cache_fill(K, V, Kc, Vc, 30, 2)), (1, lambda: psk.window_decode_step(Q[:, :, 0].contiguous(), K[:, :, 0].contiguous(), V[:, :, 0].contiguous(), Kc, Vc, pos, 30, 2)),
+                       (1, lambda: psk.layer_norm_fwd(Q)), (1, lambda: psk.layer_norm_bwd(Q, None, Q, params=False)), (2, lambda: psk.layer_norm_bwd(Q, None, Q))):
+        assert launches(lambda: psk.causal_attn_bwd(X, X, X, G, G, X, torch.ones(1, 4, 128, device="cuda"), X, 128)) == other
+        assert launches(call) == want
+    with pytest.raises(psk.PskError):
+        psk.window_attn_fwd(Q, K, V, 0)
+    assert psk.last_launch_count() == 2                   # (a refused call enqueues nothing and is not counted)
