@@ -304,7 +304,7 @@ int psk_layer_norm_bwd(const psk_norm_shape* shape, const void* X, const float* 
  *                  shape); its first word is the status that psk_check() reads.  One call's at a time: calls, and replays
  *                  of captured ones, that may run side by side take one each (as for psk_layer_norm_bwd)
  * Query head h reads key head h / (H / Hkv); dK and dV are summed over the query heads that share one, in a fixed
- * order.  h = 64, any n >= 1, window >= 1, sinks >= 0, scale > 0.  fp32 storage: CUDA cores, fp32 arithmetic.  bf16 storage: tensor
+ * order.  h = 64, any n >= 1, window >= 1, sinks >= 0, scale > 0 with scale log2(e) in fp32's range.  fp32 storage: CUDA cores, fp32 arithmetic.  bf16 storage: tensor
  * cores with fp32 accumulation, weights and their gradients rounded to bf16 once as operands (PSK_PATH_CUDA_CORES: fp32
  * arithmetic throughout), and fewer than 2^25 rows of the query heads of one key head that may see one key (n with sinks,
  * window + 128 without; PSK_ERR_UNSUPPORTED).  The backward takes D_i = do_i . o_i from the stored O. */

@@ -571,7 +571,7 @@ int check_common(const psk_window_shape* sh) {
     if (sh == nullptr) return PSK_ERR_INVALID_ARG;
     if (sh->dtype != PSK_F32 && sh->dtype != PSK_BF16) return PSK_ERR_INVALID_ARG;
     if (sh->path < PSK_PATH_AUTO || sh->path > PSK_PATH_TENSOR_CORES) return PSK_ERR_INVALID_ARG;
-    if (!(sh->scale > 0.f) || isinf(sh->scale)) return PSK_ERR_INVALID_ARG;
+    if (!(sh->scale > 0.f) || isinf(sh->scale * kLog2e)) return PSK_ERR_INVALID_ARG;      // (scores are kept times log2(e))
     if (sh->B <= 0 || sh->H <= 0 || sh->Hkv <= 0 || sh->H % sh->Hkv != 0) return PSK_ERR_SHAPE;
     if (sh->window <= 0 || sh->sinks < 0) return PSK_ERR_SHAPE;
     if ((int64_t)sh->B * sh->H >= (int64_t)1 << 31) return PSK_ERR_SHAPE;

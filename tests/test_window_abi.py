@@ -166,3 +166,13 @@ def test_extents_beyond_32_bits():
         assert e.value.code == -3
     s = psk.binding.make_window_shape(torch.zeros(1, 2, 8, 64), torch.zeros(1, 1, 8, 64), 2**31 - 1, 2**31 - 1)
     assert (s.window, s.sinks) == (2**31 - 1, 2**31 - 1)
+
+
+@pytest.mark.parametrize("scale,code", [(3.4e38, -1), (2.4e38, -1), (2.35e38, None), (1e-45, None)])
+def test_scales_at_the_ends(L, scale, code):
+    """Scores are kept times log2(e): a scale whose product with that is infinite would make NaN of a score of 0."""
+    s = window()
+    s.scale = scale
+    if code is not None:
+        assert window_calls(L, s) == (code,) * 4
+    assert (L.psk_window_workspace_bytes(byref(s), 0) == 0) == (code is not None)
