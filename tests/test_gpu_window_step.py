@@ -251,3 +251,24 @@ def test_launches_are_counted():
     with pytest.raises(psk.PskError):
         psk.window_attn_fwd(Q, K, V, 0)
     assert psk.last_launch_count() == 2                   # (a refused call enqueues nothing and is not counted)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_cache_fill_by_either_binding(dtype, monkeypatch):
+    """The native marshalling and ctypes leave the same cache, which is the one that the positions say."""
+    B, Hkv, n, window, sinks = 3, 2, 90, 33, 4
+    K, V = rand(dtype, B, Hkv, n, 64, seed=51), rand(dtype, B, Hkv, n, 64, seed=52)
+    lens = torch.tensor([n, 20, 0], dtype=torch.int32, device="cuda")
+    caches = []
+    for native in (True, False):
+        if not native:
+            monkeypatch.setattr(binding, "_fast", binding._NoNative())
+        c = tuple(torch.full((B, Hkv, sinks + window, 64), 3.0, dtype=DT[dtype], device="cuda") for _ in range(2))
+        psk.window_cache_fill(K, V, *c, window, sinks, lens)
+        caches.append(c)
+    for a, b, x in zip(*caches, (K, V)):
+        assert torch.equal(a, b)
+        for i, L in enumerate(lens.tolist()):
+            held = orc.cache_slots(window, sinks, L)
+            for slot in range(sinks + window):
+                assert torch.equal(a[i, :, slot], x[i, :, held[slot]]) if slot in held else (a[i, :, slot] == 3).all()
