@@ -307,7 +307,8 @@ int psk_layer_norm_bwd(const psk_norm_shape* shape, const void* X, const float* 
  * order.  h = 64, any n >= 1, window >= 1, sinks >= 0, scale > 0 with scale log2(e) in fp32's range.  fp32 storage: CUDA cores, fp32 arithmetic.  bf16 storage: tensor
  * cores with fp32 accumulation, weights and their gradients rounded to bf16 once as operands (PSK_PATH_CUDA_CORES: fp32
  * arithmetic throughout), and fewer than 2^25 rows of the query heads of one key head that may see one key (n with sinks,
- * window + 128 without; PSK_ERR_UNSUPPORTED).  The backward takes D_i = do_i . o_i from the stored O. */
+ * window + 128 without; PSK_ERR_UNSUPPORTED).  The backward takes D_i = do_i . o_i from the stored O; on
+ * the tensor cores the part of D that O's rounding to bf16 took is found again from the sums of the rows' p (do . v - D). */
 typedef struct {
     int32_t B, H, Hkv, n, h, window, sinks;
     int32_t dtype;              /* psk_dtype */

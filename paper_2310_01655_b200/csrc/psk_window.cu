@@ -678,7 +678,8 @@ size_t psk_window_workspace_bytes(const psk_window_shape* shape, int for_backwar
         const size_t bytes = align_up(row_sum_bytes(k)) + align_up(partial_bytes(k)) + (tile == 128 && shape->dtype == PSK_BF16 ? align_up(redo_bytes(a, &k)) : 0);
         if (bytes > sums) sums = bytes;
     }
-    return kStatusBytes + 2 * align_up((size_t)a.B * a.H * a.n * sizeof(float)) + sums;
+    const size_t rows = align_up((size_t)a.B * a.H * a.n * sizeof(float));
+    return kStatusBytes + 2 * rows + (shape->dtype == PSK_BF16 ? 2 * rows : 0) + sums;
 }
 
 int psk_window_attn_fwd(const psk_window_shape* shape, const void* Q, const void* K, const void* V, const int32_t* lengths, void* O, float* lse,
@@ -722,7 +723,8 @@ int psk_window_attn_bwd(const psk_window_shape* shape, const void* Q, const void
     a.stat_l = reinterpret_cast<float*>(static_cast<char*>(workspace) + kStatusBytes);
     a.stat_d = a.stat_l + align_up((size_t)a.B * a.H * a.n * sizeof(float)) / sizeof(float);
     WinArgs k = key_side(a, on_tensor_cores(shape) ? 128 : kTile);
-    k.rows = a.stat_d + align_up((size_t)a.B * a.H * a.n * sizeof(float)) / sizeof(float);
+    a.stat_r = a.stat_d + align_up((size_t)a.B * a.H * a.n * sizeof(float)) / sizeof(float);
+    k.rows = a.stat_r + (shape->dtype == PSK_BF16 ? 2 * align_up((size_t)a.B * a.H * a.n * sizeof(float)) / sizeof(float) : 0);
     k.partial = k.rows + align_up(row_sum_bytes(k)) / sizeof(float);
     // (first the query side's, then the key side's)
     a.redo = k.redo = reinterpret_cast<uint2*>(k.partial + align_up(partial_bytes(k)) / sizeof(float));

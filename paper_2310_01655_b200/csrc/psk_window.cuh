@@ -18,6 +18,7 @@ struct WinArgs {
     const float* lse_in;
     float* lse;
     float *stat_l, *stat_d;           // [B,H,n] scratch: -lse log2(e) and -D, written by the query side, read by the key side
+    float* stat_r;                    // [2][B,H,n] scratch of the query side on the tensor cores: sums of ds over a third of a row's steps
     const int32_t* lengths;           // [B] or null
     int* status;                      // the call's status word; its first kernel clears it (CUDA-core kernels)
     int B, H, Hkv, G, n, window, sinks;

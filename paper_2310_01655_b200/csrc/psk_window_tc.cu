@@ -4,11 +4,11 @@
 // stays: while an item's last exponentials are formed and its result is stored, the next one's operands are loaded
 // and its first scores formed.  Which item comes next the hardware says (cluster launch control: a CTA takes over
 // one of those that have not been started), so that items of different length even out.
-// With head dimension 64 a 128 x 128 tile holds the tensor pipe 512 cycles in the forward, 1014 on the query side and 1270 on the key
+// With head dimension 64 a 128 x 128 tile holds the tensor pipe 512 cycles in the forward and 1270 on either
 // side of the backward (operands read from shared memory: 48 cycles for M = 128, N = 64, K = 16, where 16 would do), and the exponential
-// unit (16 per cycle and SM) 1024 cycles in each.  It takes 1830, 2400 and 2850: what bounds it is the way from scores to
-// rows and back to the next products, under which too few other steps lie.  192 heads x 8192 rows, window 512: 413, 542 and 643 us,
-// 480, 550 and 620 TFLOP/s of the pairs that count.
+// unit (16 per cycle and SM) 1024 cycles in each.  It takes 1830, 2600 and 2850: what bounds it is the way from scores to
+// rows and back to the next products, under which too few other steps lie.  192 heads x 8192 rows, window 512: 412, 586 and 641 us,
+// 480, 510 and 620 TFLOP/s of the pairs that count.
 #include "fast_div.cuh"
 #include "packed.cuh"
 #include "tc_common.cuh"
@@ -106,17 +106,20 @@ __device__ __forceinline__ void zero_tile(bf16* p, int64_t stride, int row0, int
     }
 }
 
-// Half a row of 64 values (times f, as bf16; zeros if !live) into a staged tile; true if all of them are finite.
-__device__ __forceinline__ bool stage_half(uint8_t* st, int row, int half, uint32_t taddr, float f, bool live) {
+// Half a row of 64 values (times f, SECOND: plus another's times f1; as bf16; zeros if !live) into a staged tile; true if all of them are finite.
+template <bool SECOND = false>
+__device__ __forceinline__ bool stage_half(uint8_t* st, int row, int half, uint32_t taddr, float f, bool live, uint32_t taddr1 = 0, float f1 = 0.f) {
     f2 zero = 0;                                          // (becomes NaN with any infinity or NaN)
-    const f2 ff = pack2(f, f);
-    Cols<32> o;
+    const f2 ff = pack2(f, f), ff1 = pack2(f1, f1);
+    Cols<32> o, o1;
     o.load(taddr + half * 32);
+    if constexpr (SECOND) o1.load(taddr1 + half * 32);
     tmem_ld_wait();
     uint32_t w[16];
 #pragma unroll
     for (int j = 0; j < 32; j += 2) {
-        const f2 v = mul2(o.pair(j), ff);
+        f2 v = mul2(o.pair(j), ff);
+        if constexpr (SECOND) v = fma2(o1.pair(j), ff1, v);
         zero = fma2(v, 0ull, zero);
         w[j / 2] = live ? pack_bf16(lo2(v), hi2(v)) : 0u;
     }
@@ -126,6 +129,10 @@ __device__ __forceinline__ bool stage_half(uint8_t* st, int row, int half, uint3
 }
 __device__ __forceinline__ bool stage_row(uint8_t* st, int row, uint32_t taddr, float f, bool live) {
     const bool a = stage_half(st, row, 0, taddr, f, live), b = stage_half(st, row, 1, taddr, f, live);
+    return a && b;
+}
+__device__ __forceinline__ bool stage_row(uint8_t* st, int row, uint32_t taddr, float f, bool live, uint32_t taddr1, float f1) {
+    const bool a = stage_half<true>(st, row, 0, taddr, f, live, taddr1, f1), b = stage_half<true>(st, row, 1, taddr, f, live, taddr1, f1);
     return a && b;
 }
 // A row of 64 values times f into memory as fp32 (where `live`), for sums over parts.
@@ -507,13 +514,16 @@ struct Steps {
 
 // ---------------------------------------------------------------------------
 // Query side.  Steps of 64 keys: S = Q K^T and dP = dO V^T into tensor memory, ds = p (dP - D) as bf16 over S, dQ += ds K.
-// Every thread forms D_i = do_i . o_i of its row from the tiles in shared memory; the first warpgroup leaves -lse log2(e) and -D for the key
-// side.
+// Every thread forms D0_i = do_i . o_i of its row from the tiles in shared memory, with o as it was stored, rounded to bf16.  What that takes from D
+// shows in the sum of the row's ds, which is D - D0 (the weights sum to one), and with D0 alone it is as large as all other roundings
+// together where few keys count (windows of 8 rows: 2.6e-3 instead of 2.3e-3; of 2: 3.6e-3).  So p goes over dP as a second operand, Kb += p K,
+// and dQ = sum ds k - (D - D0) Kb; the key side gets -lse log2(e) and the whole -D.  Sixteen MMAs a step instead of twelve:
+// 192 heads x 8192 rows, window 512, 586 us instead of 538.
 // ---------------------------------------------------------------------------
 struct Dq {
     static constexpr int kMma = 12, kLoad = 13, kWarps = 14, kThreads = 32 * kWarps, kStages = 5;
     static constexpr int QGO = 0, KV = 2 * 49152, St = KV + kStages * 16384, bytes = St + kGroups * 16384 + 1024;
-    static constexpr uint32_t kTmem = 512, cDq = 0, cS = 64;                   // cS + 128 warpgroup: S (ds), dP
+    static constexpr uint32_t kTmem = 512, cDq = 0, cS = 64, cKb = 448;        // cS + 128 warpgroup: S (ds), dP (p)
 };
 
 template <bool TAKES>
@@ -526,12 +536,13 @@ tc_win_dq_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
     __shared__ __align__(16) Sched sched;
     __shared__ float s_lse[2][kRows];
     __shared__ uint32_t s_redo[4 * kGroups];
-    __shared__ uint64_t bar_q[2], free_q[2], bar_kv[Dq::kStages], free_kv[Dq::kStages], bar_s[kGroups], bar_ds[kGroups], bar_fin[4], bar_acc;
+    __shared__ uint64_t bar_q[2], free_q[2], bar_kv[Dq::kStages], free_kv[Dq::kStages], bar_s[kGroups], bar_ds[kGroups], bar_fin[4], bar_sum[4], bar_acc;
     __shared__ uint32_t tm_slot;
     const int tid = threadIdx.x, warp = warp_index(), lane = tid % 32;
     if (tid == 0) {
         cta_giveup_init();
         sched_init(sched, Dq::kWarps);
+        for (int i = 0; i < 4; ++i) mbar_init(&bar_sum[i], 4 * kGroups);
         for (int i = 0; i < 2; ++i) { mbar_init(&bar_q[i], 33); mbar_init(&free_q[i], 1 + 4 * kGroups); }
         for (int i = 0; i < Dq::kStages; ++i) { mbar_init(&bar_kv[i], 1); mbar_init(&free_kv[i], 1); }
         for (int i = 0; i < kGroups; ++i) { mbar_init(&bar_s[i], 1); mbar_init(&bar_ds[i], 4); }
@@ -550,7 +561,7 @@ tc_win_dq_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
     auto tiles_of = [&](const Item& p) { return key_tiles(p.row0, (p.row0 + kRows < p.len ? p.row0 + kRows : p.len) - 1, a.window, a.sinks, 64); };
     if (warp == Dq::kLoad) {
         bool ok = true;
-        int t = 0, items = 0;                             // items: with Q, dO, O asked for, one ahead of the keys (558 -> 542 us on 8192 rows of 192 heads)
+        int t = 0, items = 0;                             // items: with Q, dO, O asked for, one ahead of the keys (8192 rows of 192 heads 3 % faster)
         auto load_q = [&](const Item& p) {
             const int buf = items & 1;
             if (items >= 2) ok = __all_sync(0xffffffffu, mbar_wait(&free_q[buf], (items / 2 - 1) & 1, status, kErrMma));
@@ -637,6 +648,8 @@ tc_win_dq_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
                 tc_fence_after();
 #pragma unroll
                 for (int k = 0; k < 4; ++k) umma_ts(tm + Dq::cDq, tm + Dq::cS + g * 128 + k * 8, desc_off(kvd, s * 16384 + k * 2048), idesc_o, (!first || k > 0) ? 1u : 0u);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) umma_ts(tm + Dq::cKb, tm + Dq::cS + g * 128 + 64 + k * 8, desc_off(kvd, s * 16384 + k * 2048), idesc_o, (!first || k > 0) ? 1u : 0u);
                 umma_commit(&free_kv[s]);
                 if (last) umma_commit(&bar_fin[(w.started - 1) & 3]);
             };
@@ -697,11 +710,8 @@ tc_win_dq_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
                         stat.y = fmaf(__uint_as_float(gw[w] & 0xffff0000u), -__uint_as_float(ow[w] & 0xffff0000u), stat.y);
                     }
                 }
-                if (group == 0 && i < p.len) {
-                    const int64_t at = ((int64_t)p.b * a.H + p.h) * a.n + i;
-                    a.stat_l[at] = stat.x;
-                    a.stat_d[at] = stat.y;
-                }
+                const int64_t at = ((int64_t)p.b * a.H + p.h) * a.n + i, rows = (int64_t)a.B * a.H * a.n;
+                f2 sum = 0;
                 const f2 l2 = pack2(stat.x, stat.x), D2 = pack2(stat.y, stat.y);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&free_q[buf]);
@@ -715,32 +725,50 @@ tc_win_dq_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
                     for (int q = 0; q < 2; ++q) {
                         const uint32_t w = whole ? 0xffffffffu : km.word(q);
                         const Seen seen = whole ? kAll : seen_by_warp(w);
-                        if (seen == kNone) { store_zeros(tS + q * 16); continue; }
+                        if (seen == kNone) { store_zeros(tS + q * 16); store_zeros(tS + 64 + q * 16); continue; }
                         Cols<32> s, d;
                         s.load(tS + q * 32);
                         d.load(tS + 64 + q * 32);
                         tmem_ld_wait();
                         // (a weight of 0 times an infinity in dP is NaN, and the row is formed again)
                         if (seen == kSome) mask_scores(s, w);
-                        uint32_t pk[16];
+                        uint32_t pk[16], dk[16];
 #pragma unroll
                         for (int j = 0; j < 32; j += 2) {
-                            const f2 ds = mul2(exp2_pair(fma2(s.pair(j), c2, l2)), add2(d.pair(j), D2));
-                            pk[j / 2] = pack_bf16(lo2(ds), hi2(ds));
+                            const f2 pr = exp2_pair(fma2(s.pair(j), c2, l2)), ds = mul2(pr, add2(d.pair(j), D2));
+                            sum = add2(sum, ds);
+                            pk[j / 2] = pack_bf16(lo2(pr), hi2(pr));
+                            dk[j / 2] = pack_bf16(lo2(ds), hi2(ds));
                         }
-                        tmem_st16(tS + q * 16, pk);
+                        tmem_st16(tS + q * 16, dk);
+                        tmem_st16(tS + 64 + q * 16, pk);
                     }
                     tmem_st_wait();
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&bar_ds[group]);
                 }
-                if ((end - 1) % kGroups == group) {       // the warpgroup with the last step finishes the item
+                // The warpgroup with the last step finishes the item; the others leave it their sums of ds (which steps those are of depends on the
+                // distance from the last step alone, and so does their order).  A warpgroup may be two items ahead of another, not three (it would need
+                // an answer of the scheduler that the other has not taken yet): hence four barriers, as for the products.
+                const int behind = (group - (end - 1) % kGroups + kGroups) % kGroups;        // 0: it finishes, 2: the step before the last
+                float r = lo2(sum) + hi2(sum);
+                if (behind > 0 && i < p.len) a.stat_r[(behind - 1) * rows + at] = r;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bar_sum[items & 3]);
+                if (behind == 0) {
                     if (row == 0) bulk_wait_read();
+                    ok = mbar_wait(&bar_sum[items & 3], (items / 4) & 1, status, kErrMma) && ok;
+                    if (ok && i < p.len) {
+                        r += a.stat_r[rows + at] + a.stat_r[at];
+                        r = finite(r) ? r : 0.f;          // (an infinity in a pair that does not count is in it too)
+                        a.stat_l[at] = stat.x;
+                        a.stat_d[at] = stat.y -= r;
+                    }
                     ok = mbar_wait(&bar_fin[items & 3], (items / 4) & 1, status, kErrMma) && ok;
                     tc_fence_after();
                     bar_sync(1 + group, kRows);
-                    const bool live = i < p.len, fine = stage_row(st, row, lane_tm + Dq::cDq, a.scale, live);
+                    const bool live = i < p.len, fine = stage_row(st, row, lane_tm + Dq::cDq, a.scale, live, lane_tm + Dq::cKb, -r * a.scale);
                     tc_fence_before();
                     const unsigned bad = __ballot_sync(0xffffffffu, ok && !fine && live && stat.x == stat.x && stat.y == stat.y);      // (with a NaN there the row is NaN)
                     if (lane == 0) mbar_arrive(&bar_acc);

@@ -447,3 +447,37 @@ def test_windows_beyond_32_bits():
         for call in (lambda: psk.window_decode_step(q, k, v, Kc, Vc, pos, window, sinks), lambda: psk.window_cache_fill(K, V, Kc, Vc, window, sinks)):
             with pytest.raises((psk.PskError, ValueError)):
                 call()
+
+
+@pytest.mark.parametrize("B,H,Hkv,n,window,sinks,lengths", [
+    (1, 2, 2, 200, 1, 0, None), (1, 2, 1, 200, 2, 0, None), (2, 2, 2, 333, 3, 1, [333, 70]), (1, 4, 2, 300, 8, 0, None), (1, 2, 2, 260, 40, 2, None), (1, 1, 1, 400, 400, 0, None),
+    (30, 8, 4, 150, 2, 0, None)])
+def test_the_rounding_of_the_stored_output_does_not_reach_the_gradients(B, H, Hkv, n, window, sinks, lengths):
+    """bf16 on the tensor cores.  D0 = do . o from the stored o is off by R = D - D0, |R| <= |do| . (o's error); with few keys to a row that is as large as
+    ds itself.  The kernels take it out again, R being the sum of the row's p (dP - D0), off by
+    eR = (ep + (N + 8) u) sum p |dP - D0| + 64 u sum p |do||v|.  Then dQ sums ds' = p (dP - D0) and p, each rounded once (e), the latter times R; dK sums ds
+    formed with D0 + R: errors |ds| (ep + e) + p |R| 2 e + p eR (+ 64 u p |do||v| and the sums' N u), times |k|; without p |R| 2 e times |q|."""
+    Q, K, V, dO = make("bf16", B, H, Hkv, n, seed=n + window)
+    lens = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    O, lse, dQ, dK, dV = run(Q, K, V, dO, window, sinks, lengths=lens)
+    e, G = E["bf16"], H // Hkv
+    for b, hk in {(0, 0), (B - 1, Hkv - 1)}:
+        k, v = f64(K[b, hk]), f64(V[b, hk])
+        dk, tk = np.zeros((n, 64)), np.zeros((n, 64))
+        for h in range(hk * G, hk * G + G):
+            q, d, L = f64(Q[b, h]), f64(dO[b, h]), None if lengths is None else lengths[b]
+            M = orc.visible(n, window, sinks, L)
+            o, _, P = orc.window_attention(q, k, v, window, sinks, 0.125, L)
+            rq, rk, _ = orc.window_attention_backward(q, k, v, d, window, sinks, 0.125, L)
+            N = M.sum(1, keepdims=True) + 64
+            ep = 2 * 68 * U * np.where(M, np.abs(q) @ np.abs(k).T, 0).max(1, keepdims=True) * 0.125 + 2.0 ** -21
+            dp, D, dv = np.where(M, d @ v.T, 0), (d * o).sum(1, keepdims=True), np.where(M, np.abs(d) @ np.abs(v).T, 0)
+            R = (np.abs(d) * ((ep + e + N * U) * (P @ np.abs(v)) + e * np.abs(o))).sum(1, keepdims=True) + 64 * U * (np.abs(d) * np.abs(o)).sum(1, keepdims=True)
+            ds = np.abs(P * (dp - D))
+            eR = (ep + (N + 8) * U) * (ds + P * R).sum(1, keepdims=True) + 64 * U * (P * dv).sum(1, keepdims=True)
+            both = ds * (ep + e + 4 * U) + P * (eR + 64 * U * dv + 4 * U * np.abs(D))
+            eq = both + P * R * (2 * e + ep)
+            within("dQ[%d,%d]" % (b, h), dQ[b, h], rq, 0.125 * (eq + N * U * (ds + P * R + eq)) @ np.abs(k) + (e + 2 * U) * np.abs(rq))
+            dk += rk
+            tk += 0.125 * (both.T @ np.abs(q) + (M.sum(0)[:, None] * G + 64) * U * ((ds + both).T @ np.abs(q)))
+        within("dK[%d,%d]" % (b, hk), dK[b, hk], dk, tk + (e + 2 * U) * (np.abs(dk) + tk))
