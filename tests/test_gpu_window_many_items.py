@@ -45,3 +45,31 @@ def test_many_items_of_one_row():
     assert torch.equal(O, V.repeat_interleave(3, 1)) and ((lse - s).abs() <= 2.0 ** -14 * (1 + s.abs())).all()
     want = dO.double().view(100, 8, 3, 1, 64).sum(2)
     assert ((dV.double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -18 * dO.double().view(100, 8, 3, 1, 64).abs().sum(2)).all()
+
+
+def test_many_items_captured_and_beside_one_another():
+    """Replayed from a graph with other inputs, and on two streams at once."""
+    sets = [make("bf16", 8, H, 4, N, seed=60 + i) for i in range(2)]
+    lens = torch.tensor([N, 0, 300, N, 1, 128, 0, 777], dtype=torch.int32, device="cuda")
+    step = lambda Q, K, V, dO: (lambda O, lse: (O, lse) + psk.window_attn_bwd(Q, K, V, O, lse, dO, 150, 3, lengths=lens))(*psk.window_attn_fwd(Q, K, V, 150, 3, lengths=lens))
+    refs = [step(*s) for s in sets]
+    torch.cuda.synchronize()
+    held = [x.clone() for x in sets[0]]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(*held)
+    for s, ref in zip((sets[1], sets[0]), (refs[1], refs[0])):
+        for x, y in zip(held, s):
+            x.copy_(y)
+        for _ in range(3):
+            graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(got, ref))
+    streams, outs = [torch.cuda.Stream() for _ in sets], [[], []]
+    for _ in range(5):
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                outs[i].append(step(*sets[i]))
+    torch.cuda.synchronize()
+    for ref, some in zip(refs, outs):
+        assert all(torch.equal(x, y) for one in some for x, y in zip(one, ref))
