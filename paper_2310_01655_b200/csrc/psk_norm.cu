@@ -5,10 +5,10 @@
 // Bound: memory.  A row is read once and stays in registers; the backward forms mean and rstd again from the x that it
 // reads anyway, so that nothing but x is kept from the forward (for rows of 64 in bf16 two stored floats would be 6 % of
 // the forward's bytes).  All sums in fp32, the variance from the deviations (two passes over registers).
-// A row belongs to G = 4 to 32 lanes of a warp, or to a CTA; which, by how many 16-byte accesses it has (a lane keeps 8 to 32
+// A row belongs to G = 4 to 32 lanes of a warp, to 2 or 4 warps, or to a CTA; which, by how many accesses it has (a lane keeps up to 32
 // values: a row's own work, its addresses, its sums over lanes, its root, is shared by few lanes).  The next row is on its way while one is
 // worked on.  Values are handled in packed pairs: with scalar arithmetic the issue slots bound the backward of rows of 64 (1.57 M rows: 236 us).
-// Rows whose address or stride is not a multiple of 16 bytes are read value by value.
+// Rows whose address or stride is not a multiple of 16 bytes are read by two values, and those of odd length, stride or start value by value.
 #include "fast_div.cuh"
 #include "packed.cuh"
 #include "psk_internal.cuh"
