@@ -298,7 +298,8 @@ int psk_layer_norm_bwd(const psk_norm_shape* shape, const void* X, const float* 
  *   Q, O, dO, dQ   DEVICE [B, H, n, h], strides q_stride_*;  K, V, dK, dV   DEVICE [B, Hkv, n, h], strides kv_stride_*
  *                  (elements, last dimension contiguous, multiples of 16 bytes; the stride of an extent of 1 is not
  *                  looked at); rows must not overlap (PSK_ERR_SHAPE), outputs overlap no input
- *   lse            DEVICE [B, H, n] fp32, written by the forward, read by the backward
+ *   lse            DEVICE [B, H, n] fp32, written by the forward, read by the backward; O and lse reach the backward as the forward left them
+ *                  for the same Q, K, V (it relies on a row's weights summing to one)
  *   lengths        DEVICE [B] int32 or NULL (all n); clamped to 0 .. n
  *   workspace      DEVICE scratch, 256-byte aligned, >= psk_window_workspace_bytes(shape, for_backward) (0 for a bad
  *                  shape); its first word is the status that psk_check() reads.  One call's at a time: calls, and replays

@@ -752,7 +752,7 @@ def window_attn_fwd(Q, K, V, window, sinks=0, scale=None, lengths=None, path=PAT
 
 
 def window_attn_bwd(Q, K, V, O, lse, dO, window, sinks=0, scale=None, lengths=None, path=PATH_AUTO, workspace=None, out=None):
-    """psk_window_attn_bwd: returns (dQ, dK, dV) from the forward's inputs and outputs."""
+    """psk_window_attn_bwd: returns (dQ, dK, dV) from the forward's inputs and its outputs O and lse as they were."""
     res = (_fast or _native()).window_attn_bwd(Q, K, V, O, lse, dO, window, sinks, 0.125 if scale is None else scale, lengths, path, workspace, out)
     if res is not None:
         return _result(res, "psk_window_attn_bwd")
