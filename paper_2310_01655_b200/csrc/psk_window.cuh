@@ -70,7 +70,12 @@ __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0
 // the row NaN.  In the tensor-core kernels waits have a limit of a second, and a row over a long sequence takes a warp longer: there such rows
 // are only noted, and looked at when nobody in the CTA waits any more.
 constexpr int kRedo = 8;
-template <typename T> __device__ __forceinline__ float2 ld2(const T* p) { return make_float2(ldf(p), ldf(p + 1)); }
+// (p: of an even column, of a row on 16 bytes)
+__device__ __forceinline__ float2 ld2(const float* p) { return *reinterpret_cast<const float2*>(p); }
+__device__ __forceinline__ float2 ld2(const bf16* p) {
+    const uint32_t u = *reinterpret_cast<const uint32_t*>(p);
+    return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+}
 template <typename T> __device__ __forceinline__ void st2(T* p, float2 v) { stf(p, v.x); stf(p + 1, v.y); }
 __device__ __forceinline__ float dot2(float2 a, float2 b) { return fmaf(a.x, b.x, a.y * b.y); }
 __device__ __forceinline__ bool all_nan(float2 v) { return __all_sync(0xffffffffu, v.x != v.x && v.y != v.y); }
@@ -128,15 +133,21 @@ __device__ __noinline__ float2 redo_out_row(const T* q, const T* K, const T* V, 
             v[u] = ld2(V + at);
         }
         warp_sums(s);
+        float top = m;                                    // (a NaN score: p is NaN, and so is the row)
+#pragma unroll
+        for (int u = 0; u < kRedo; ++u) { s[u] *= c; top = t + u < count ? fmaxf(top, s[u]) : top; }
+        const float base = top == neg_inf() ? 0.f : top, alpha = exp2_approx(m - base);
+        acc.x *= alpha;
+        acc.y *= alpha;
+        l *= alpha;
+        m = top;
 #pragma unroll
         for (int u = 0; u < kRedo; ++u) {
             if (t + u >= count) break;
-            const float x = s[u] * c, m2 = fmaxf(m, x);   // (a NaN score: p is NaN, and so is the row)
-            const float base = m2 == neg_inf() ? 0.f : m2, alpha = exp2_approx(m - base), p = exp2_approx(x - base);
-            acc.x = fmaf(acc.x, alpha, p * v[u].x);
-            acc.y = fmaf(acc.y, alpha, p * v[u].y);
-            l = fmaf(l, alpha, p);
-            m = m2;
+            const float p = exp2_approx(s[u] - base);
+            acc.x = fmaf(p, v[u].x, acc.x);
+            acc.y = fmaf(p, v[u].y, acc.y);
+            l += p;
         }
     }
     return make_float2(acc.x / l, acc.y / l);
